@@ -238,6 +238,66 @@ MAXK_API maxk_status maxk_cbsr_scatter(const float* d_values, const void* d_sp_i
  */
 MAXK_API maxk_status spmm_baseline(maxk_graph* g, const float* d_H, int32_t dim, float* d_Y, void* stream);
 
+/*
+ * Microscaled storage of dense matrices: the linear half of a layer, X W^T + b, whose input X training keeps for the
+ * weight gradient.  A row of din columns is cut into nb = ceil(din / 32) blocks of 32 columns, the last one filled up with zeros; a
+ * block has one scale byte s, a power of two.
+ *   MAXK_MX_8  codes int8  [N x 32 nb], in [-127, 127]:  value = code * 2^(s - 133)
+ *   MAXK_MX_4  codes uint8 [N x 16 nb], two 4-bit codes a byte, the even column in the low half; a code is a sign (bit 3) and a
+ *              magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0 to 2):  value = sign * magnitude * 2^(s - 127)
+ *   scales uint8 [N x nb];  s = 255: the block stands for NaN.
+ * Code arrays are 16-byte aligned.  Either format holds at most 8 significant bits, so its values are exact in bf16.
+ * Beyond the conventions above: widths are at most MAXK_MX_MAX_DIM (MAXK_UNSUPPORTED), N below 2^31 - 15, and a gradient dH
+ * comes dense (row-major [N x dout] of a MAXK_VALUE_* format) or, in the *_cbsr calls, as maxk_sspmm_bwd leaves it:
+ * d_dXs fp32 [N x k] at the distinct columns sp_index [N x k] below dout, zeros elsewhere.  These calls need no maxk_graph, allocate
+ * nothing and may be captured into a HIP graph.  Products with a non-finite operand give non-finite sums, as they do in a
+ * dense product (Inf may become NaN).
+ */
+enum { MAXK_MX_8 = 0, MAXK_MX_4 = 1 };
+#define MAXK_MX_MAX_DIM 65536
+
+/*
+ * X [N x din] (a MAXK_VALUE_* format) into codes and scales: s is the exponent field of the block's largest magnitude (less 2, and at
+ * least 0, for MAXK_MX_4), codes are rounded to nearest, halfway cases to even, and saturate.  A block with an Inf or NaN stands
+ * for NaN.  And back: values rounded once to the format of X where it holds fewer bits.
+ */
+MAXK_API maxk_status maxk_mx_quantize(const void* d_X, int32_t value_type, int64_t N, int32_t din, int32_t format, void* d_codes,
+                                      uint8_t* d_scales, void* stream);
+MAXK_API maxk_status maxk_mx_dequantize(const void* d_codes, const uint8_t* d_scales, int32_t format, int64_t N, int32_t din, void* d_X,
+                                        int32_t value_type, void* stream);
+
+/*
+ * Y[n,o] = bias[o] + sum_i X[n,i] W[o,i], X [N x din] and W [dout x din] both MAXK_MX_4, fp32 sums, Y [N x dout] in a
+ * MAXK_VALUE_* format (rounded once).  d_bias is fp32 [dout] or NULL.
+ */
+MAXK_API maxk_status maxk_mx_linear(const uint8_t* d_x_codes, const uint8_t* d_x_scales, int64_t N, const uint8_t* d_w_codes,
+                                    const uint8_t* d_w_scales, int32_t din, int32_t dout, const float* d_bias, void* d_Y,
+                                    int32_t value_type, void* stream);
+
+/*
+ * Weight gradient from a checkpoint: dW[o,i] = sum_n dH[n,o] X[n,i], fp32 [dout x din], and db[o] = sum_n dH[n,o], fp32 [dout]
+ * (d_db NULL: not computed).  X in either format.  Sums run in fp32 over ranges of rows, whose sums are then added up in a fixed order: the same call
+ * gives the same bits.  d_workspace holds maxk_mx_weight_grad_workspace(N, din, dout) bytes (16-byte aligned; never 0), and may be used
+ * again by later work on the stream.  MAXK_SCRATCH_TOO_SMALL where workspace_bytes is less.
+ */
+MAXK_API int64_t maxk_mx_weight_grad_workspace(int64_t N, int32_t din, int32_t dout);
+MAXK_API maxk_status maxk_mx_weight_grad(const void* d_codes, const uint8_t* d_scales, int32_t format, int64_t N, int32_t din, int32_t dout,
+                                         const void* d_dH, int32_t value_type, float* d_dW, float* d_db, void* d_workspace,
+                                         int64_t workspace_bytes, void* stream);
+MAXK_API maxk_status maxk_mx_weight_grad_cbsr(const void* d_codes, const uint8_t* d_scales, int32_t format, int64_t N, int32_t din,
+                                              int32_t dout, const float* d_dXs, const void* d_sp_index, int32_t index_bytes, int32_t k,
+                                              float* d_dW, float* d_db, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Input gradient: dX[n,i] = sum_o dH[n,o] W[o,i], W [dout x din] MAXK_MX_4, fp32 sums, dX [N x din] in a MAXK_VALUE_* format (rounded
+ * once).
+ */
+MAXK_API maxk_status maxk_mx_input_grad(const void* d_dH, int32_t value_type, int64_t N, const uint8_t* d_w_codes, const uint8_t* d_w_scales,
+                                        int32_t din, int32_t dout, void* d_dX, int32_t dx_value_type, void* stream);
+MAXK_API maxk_status maxk_mx_input_grad_cbsr(const float* d_dXs, const void* d_sp_index, int32_t index_bytes, int32_t k, int64_t N,
+                                             const uint8_t* d_w_codes, const uint8_t* d_w_scales, int32_t din, int32_t dout, void* d_dX,
+                                             int32_t dx_value_type, void* stream);
+
 /* Text for a status code (static storage). */
 MAXK_API const char* maxk_status_string(maxk_status s);
 

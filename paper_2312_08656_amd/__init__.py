@@ -33,4 +33,18 @@ from .binding import (  # noqa: F401
     maxk_topk_cbsr_narrow,
     spmm_baseline,
 )
+from .mx import (  # noqa: E402,F401
+    MX_4,
+    MX_8,
+    maxk_mx_dequantize,
+    maxk_mx_input_grad,
+    maxk_mx_input_grad_cbsr,
+    maxk_mx_linear,
+    maxk_mx_quantize,
+    maxk_mx_weight_grad,
+    maxk_mx_weight_grad_cbsr,
+    mx_blocks,
+    mx_empty,
+    mx_weight_grad_workspace,
+)
 from .autograd import MaxKAggregate, maxk_aggregate  # noqa: E402,F401

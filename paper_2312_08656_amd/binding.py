@@ -26,6 +26,8 @@ EXPORTS = (
     "maxk_graph_regs_tables", "maxk_graph_regs_stands_in", "maxk_regs_step_list", "maxk_graph_regs_table",
     "maxk_graph_limit_allocations", "maxk_expand_past_l2", "maxk_scatter_past_l2", "maxk_lone_visit_line",
     "maxk_entry_batch", "maxk_fwd_by_units", "maxk_pull_by_units",
+    "maxk_mx_quantize", "maxk_mx_dequantize", "maxk_mx_linear", "maxk_mx_weight_grad_workspace", "maxk_mx_weight_grad",
+    "maxk_mx_weight_grad_cbsr", "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr",
 )
 
 
@@ -101,6 +103,18 @@ def load_library() -> ctypes.CDLL:
     lib.maxk_fwd_by_units.restype = i32
     lib.maxk_pull_by_units.argtypes = [i32, i32, i32, i64, i64, ctypes.c_double]
     lib.maxk_pull_by_units.restype = i32
+    lib.maxk_mx_quantize.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+    lib.maxk_mx_dequantize.argtypes = [vp, vp, i32, i64, i32, vp, i32, vp]
+    lib.maxk_mx_linear.argtypes = [vp, vp, i64, vp, vp, i32, i32, vp, vp, i32, vp]
+    lib.maxk_mx_weight_grad_workspace.argtypes = [i64, i32, i32]
+    lib.maxk_mx_weight_grad_workspace.restype = i64
+    lib.maxk_mx_weight_grad.argtypes = [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, i64, vp]
+    lib.maxk_mx_weight_grad_cbsr.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, i32, i32, vp, vp, vp, i64, vp]
+    lib.maxk_mx_input_grad.argtypes = [vp, i32, i64, vp, vp, i32, i32, vp, i32, vp]
+    lib.maxk_mx_input_grad_cbsr.argtypes = [vp, vp, i32, i32, i64, vp, vp, i32, i32, vp, i32, vp]
+    for name in ("maxk_mx_quantize", "maxk_mx_dequantize", "maxk_mx_linear", "maxk_mx_weight_grad", "maxk_mx_weight_grad_cbsr",
+                 "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr"):
+        getattr(lib, name).restype = i32
     lib.maxk_last_hip_error.argtypes = []
     lib.maxk_version.argtypes = []
     _LIB = lib
