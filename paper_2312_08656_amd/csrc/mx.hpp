@@ -16,6 +16,12 @@ __device__ __forceinline__ float mx_scale(uint32_t s)
     return __uint_as_float(s == 0 ? 0x00400000u : s == 255 ? 0x7FC00000u : s << 23);
 }
 
+// 2^(s - 133), what a whole step of an 8-bit code is worth (subnormal below s = 7); s = 255: NaN
+__device__ __forceinline__ float mx8_unit(uint32_t s)
+{
+    return __uint_as_float(s >= 7 ? (s == 255 ? 0x7FC00000u : (s - 6) << 23) : 0x00800000u >> (7 - s));
+}
+
 // magnitude of a 4-bit code: its two exponent bits and its last bit moved to their places in a float with a bias of 127, which is
 // 2^126 too small; exact for the subnormal 0.5 as well.  `code` may have higher bits set
 __device__ __forceinline__ float mx_e2m1(uint32_t code)
