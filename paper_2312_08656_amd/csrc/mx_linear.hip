@@ -1,21 +1,258 @@
 // Y = X W^T + b of 4-bit operands (include/maxk.h).
+//
+// The matrix instruction takes 4-bit codes with a scale byte for 32 products: 16 x 16 outputs over 128 columns, a lane holding one block of
+// either operand.  Rows are many and widths small, so a wavefront keeps 64 rows of W (all their columns) in its registers and walks
+// over the rows of X, 16 at a time; the next 16 are on their way meanwhile.  Wavefronts that share rows of X lie in one workgroup, so X is read through L1.
+#include <algorithm>
+
 #include "mx.hpp"
 
 namespace maxk {
 namespace {
 
-// one thread an output
-template <int VT>
-__global__ void linear_kernel(MxMatrix X, int64_t N, MxMatrix W, int din, int dout, const float* bias, value_store_t<VT>* Y)
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kTileRows = 16;     // rows of X in a step
+constexpr int kGroup = 64;        // columns of Y (rows of W) of a wavefront
+constexpr int kTiles = kGroup / 16;
+constexpr int kChunkBlocks = 4;   // blocks of 32 columns that an instruction takes: one for each 16 lanes
+
+template <int BYTE>  // of the scale registers
+__device__ __forceinline__ f32x4 mfma(const uint4& a, uint32_t sa, const uint4& b, uint32_t sb, f32x4 c)
 {
-    const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (at >= N * dout) return;
-    const int64_t row = at / dout;
-    const int o = (int)(at % dout), nb = mx_blocks(din);
-    float sum = 0.f;
-    for (int i = 0; i < din; ++i)
-        sum += mx_value<MAXK_MX_4>(X.codes, X.scales, row, i, nb) * mx_value<MAXK_MX_4>(W.codes, W.scales, o, i, nb);
-    Y[at] = narrow_value<VT>(bias ? sum + bias[o] : sum);
+    const i32x8 A = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, B = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);  // 4: E2M1
+}
+
+template <int C>
+struct Blocks {  // one lane's blocks of a row
+    uint4 code[C];
+    uint32_t scale[(C + 3) / 4];  // a byte each
+};
+template <int C>
+struct Loaded {
+    uint4 code[C];
+    uint32_t scale[C];
+};
+template <int C>
+__device__ __forceinline__ Blocks<C> packed(const Loaded<C>& x)
+{
+    Blocks<C> y;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        y.code[c] = x.code[c];
+        y.scale[c / 4] = c % 4 ? y.scale[c / 4] | x.scale[c] << (8 * (c % 4)) : x.scale[c];
+    }
+    return y;
+}
+
+// sum + the products of all blocks
+template <int C, int c = 0>
+__device__ __forceinline__ f32x4 products(const Blocks<C>& a, const Blocks<C>& b, f32x4 sum)
+{
+    if constexpr (c < C) return products<C, c + 1>(a, b, mfma<c % 4>(a.code[c], a.scale[c / 4], b.code[c], b.scale[c / 4], sum));
+    else return sum;
+}
+
+// Blocks g, 4 + g, ... of row `row` of those from `first` on.  Past its end: the last block again for X, zeros for W, whose products are
+// then 0 (or NaN where that block of X stands for NaN, and the row's sums with it).
+template <int C, bool ZERO>
+__device__ __forceinline__ void load_blocks(Loaded<C>& x, const MxMatrix& A, int64_t first, int row, int g, int nb)
+{
+    const uint8_t *codes = A.codes + first * nb * 16, *scales = A.scales + first * nb;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int b = c * kChunkBlocks + g, at = row * nb + min(b, nb - 1);
+        x.code[c] = *reinterpret_cast<const uint4*>(codes + (uint32_t)at * 16u);
+        x.scale[c] = scales[(uint32_t)at];
+        if (ZERO && b >= nb) x.code[c] = make_uint4(0, 0, 0, 0), x.scale[c] = 127;
+    }
+}
+
+__device__ __forceinline__ void local_barrier()  // orders LDS only: loads and stores of memory stay under way
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+constexpr int kMaxGroups = 6;     // of a workgroup: up to 384 columns of Y
+constexpr int kPad = 4;           // floats at the end of a row in LDS, so that rows begin in different banks
+
+// A workgroup makes 16 m rows of Y, up to 384 columns of each, in a step: `gcols` wavefronts side by side, m below each other.  The matrix
+// instruction leaves four columns a lane over 16 rows; the outputs are turned round in LDS and leave as whole rows.  (As they are, 64 bytes of 16 rows a
+// store: 989 us for 2.4 M rows, 256 to 256 columns; through LDS, 256 bytes of 4 rows: 666.)
+// WIDE: rows of Y are whole 16-byte pieces from a 16-byte boundary; else a column a lane.
+// ONCE: Y passes by L2.
+template <int C, int VT, bool WIDE, bool ONCE>
+__global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int64_t N, MxMatrix W, int nb, int dout, int gcols, int m,
+                                                                 const float* __restrict__ bias, value_store_t<VT>* __restrict__ Y)
+{
+    extern __shared__ __align__(16) float turned[];
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int threads = 64 * gcols * m, left = blockIdx.y * gcols * kGroup, cols = min(gcols * kGroup, dout - left);
+    const int first = left + wave % gcols * kGroup, pitch = gcols * kGroup + kPad, rows_step = kTileRows * m;
+    const int64_t steps = (N + rows_step - 1) / rows_step;
+
+    Blocks<C> w[kTiles];
+    f32x4 start[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        Loaded<C> row;
+        load_blocks<C, true>(row, W, first, min(t * 16 + r, dout - 1 - first), g, nb);
+        w[t] = packed(row);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int o = first + t * 16 + g * 4 + j;
+            start[t][j] = bias && o < dout ? bias[o] : 0.f;
+        }
+    }
+    // The pieces of a whole step that this thread stores.  Every thread makes as many stores, the spare ones of the last piece again, so that
+    // the number of stores behind a load is known and a load can be waited for without them.
+    constexpr int V = WIDE ? 16 / (int)sizeof(value_store_t<VT>) : 1, S = WIDE ? 16 / V : 1;
+    const int pieces = (cols + V - 1) / V;
+    int from[S], to[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const int q = min((int)threadIdx.x + i * threads, rows_step * pieces - 1), row = q / pieces, col = (q - row * pieces) * V;
+        from[i] = row * pitch + col;
+        to[i] = row * dout + col;
+    }
+    const int below = wave / gcols * kTileRows;
+    const auto load = [&](Loaded<C>& x, int64_t step) {
+        const int64_t row = min(min(step, steps - 1) * rows_step + below, N - 1);
+        load_blocks<C, false>(x, X, row, min(r, (int)min(N - 1 - row, (int64_t)kTileRows - 1)), g, nb);
+    };
+    Loaded<C> next;
+    load(next, blockIdx.x);
+    float* room = turned;
+    float* other = turned + rows_step * pitch;
+    int64_t step = blockIdx.x;
+    const auto make = [&]() {  // the outputs of a step, in `room`
+        const Blocks<C> x = packed(next);
+        load(next, step + gridDim.x);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+            *reinterpret_cast<f32x4*>(room + (below + r) * pitch + wave % gcols * kGroup + t * 16 + g * 4) = products(w[t], x, start[t]);
+        local_barrier();  // the room of the step before was read before the one barrier, and is written after the next
+    };
+    const auto whole_step = [&]() {
+        make();
+        value_store_t<VT>* out = Y + step * rows_step * dout + left;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            f32x4 y = *reinterpret_cast<const f32x4*>(room + from[i]);
+            if constexpr (VT != MAXK_VALUE_F32) {
+                const f32x4 z = *reinterpret_cast<const f32x4*>(room + from[i] + 4);
+                const auto two = [](float a, float b) { return __uint_as_float((uint32_t)narrow_value<VT>(a) | (uint32_t)narrow_value<VT>(b) << 16); };
+                y = f32x4{two(y[0], y[1]), two(y[2], y[3]), two(z[0], z[1]), two(z[2], z[3])};
+            }
+            f32x4* p = reinterpret_cast<f32x4*>(out + to[i]);
+            if constexpr (ONCE) __builtin_nontemporal_store(y, p);
+            else *p = y;
+        }
+        float* const swap = room;
+        room = other, other = swap;
+        step += gridDim.x;
+    };
+    if constexpr (WIDE) {
+        const int64_t whole = N / rows_step;
+        if (step < whole) {
+            whole_step();  // by itself: its loads have no stores behind them, and the loop's wait would be the same for both
+            while (step < whole) whole_step();
+        }
+    }
+    for (; step < steps; step += gridDim.x) {
+        make();
+        const int64_t row0 = step * rows_step;
+        const int rows = (int)min(N - row0, (int64_t)rows_step);
+        for (int row = wave; row < rows; row += gcols * m)
+            for (int col = lane; col < cols; col += 64) Y[(row0 + row) * dout + left + col] = narrow_value<VT>(room[row * pitch + col]);
+        float* const swap = room;
+        room = other, other = swap;
+    }
+}
+
+// Rows wider than the registers hold: 64 rows of X by 64 of W a wavefront, blocks of either straight from memory.
+template <int VT>
+__global__ void __launch_bounds__(256) linear_long_kernel(MxMatrix X, int64_t N, MxMatrix W, int nb, int dout, int groups, const float* __restrict__ bias,
+                                                          value_store_t<VT>* __restrict__ Y)
+{
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = (int)(wave % groups) * kGroup;
+    const int64_t row0 = wave / groups * 64;
+    if (row0 >= N) return;
+    f32x4 sum[4][kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const int o = first + t * 16 + r;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) sum[m][t] = bias && o < dout ? f32x4{bias[o], bias[o], bias[o], bias[o]} : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int c = 0; c < nb; c += kChunkBlocks) {
+        Blocks<1> x[4], w[kTiles];
+        const int b = min(c + g, nb - 1);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int64_t at = min(row0 + m * 16 + r, N - 1) * nb + b;
+            x[m].code[0] = *reinterpret_cast<const uint4*>(X.codes + at * 16);
+            x[m].scale[0] = X.scales[at];
+            const int64_t wt = (int64_t)min(first + m * 16 + r, dout - 1) * nb + b;
+            w[m].code[0] = *reinterpret_cast<const uint4*>(W.codes + wt * 16);
+            w[m].scale[0] = W.scales[wt];
+            if (c + g >= nb) w[m].code[0] = make_uint4(0, 0, 0, 0), w[m].scale[0] = 127;
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) sum[m][t] = products(x[m], w[t], sum[m][t]);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t row = row0 + m * 16 + g * 4 + j;
+                const int o = first + t * 16 + r;
+                if (row < N && o < dout) Y[row * dout + o] = narrow_value<VT>(sum[m][t][j]);
+            }
+}
+
+// 3 for each of the 1024 SIMDs.  2.4 M rows, 256 to 256, fp32 Y: 833 / 665 / 655 / 648 us at 1 to 4; 29 k rows, 256 to 128, fp16: 7.4 at 2, 8.3, 9.6
+constexpr int64_t kWaves = 3072;
+
+template <int C, int VT>
+void launch_chunks(const MxMatrix& X, int64_t N, const MxMatrix& W, int nb, int dout, const float* bias, value_store_t<VT>* Y, hipStream_t s)
+{
+    const int groups = (dout + kGroup - 1) / kGroup, sides = (groups + kMaxGroups - 1) / kMaxGroups, gcols = (groups + sides - 1) / sides, m = std::max(1, 4 / gcols);
+    const int64_t steps = (N + kTileRows * m - 1) / (kTileRows * m), blocks = std::min(steps, std::max<int64_t>(1, kWaves / (gcols * m * sides)));
+    const size_t lds = 2 * sizeof(float) * (size_t)(kTileRows * m) * (gcols * kGroup + kPad);
+    const dim3 grid((unsigned)blocks, (unsigned)sides), block(64 * gcols * m);
+#define MAXK_LINEAR(WIDE, ONCE) hipLaunchKernelGGL((linear_kernel<C, VT, WIDE, ONCE>), grid, block, lds, s, X, N, W, nb, dout, gcols, m, bias, Y)
+    if (dout * sizeof(*Y) % 16 != 0 || !aligned(Y, 16)) MAXK_LINEAR(false, false);
+    else if (past_l2(N * dout * (int64_t)sizeof(*Y))) MAXK_LINEAR(true, true);
+    else MAXK_LINEAR(true, false);
+#undef MAXK_LINEAR
+}
+
+template <int VT>
+maxk_status launch(const MxMatrix& X, int64_t N, const MxMatrix& W, int din, int dout, const float* bias, value_store_t<VT>* Y, hipStream_t s)
+{
+    const int nb = mx_blocks(din), chunks = (nb + kChunkBlocks - 1) / kChunkBlocks;
+    if (chunks <= 1) launch_chunks<1, VT>(X, N, W, nb, dout, bias, Y, s);
+    else if (chunks <= 2) launch_chunks<2, VT>(X, N, W, nb, dout, bias, Y, s);
+    else if (chunks <= 4) launch_chunks<4, VT>(X, N, W, nb, dout, bias, Y, s);
+    else if (chunks <= 8) launch_chunks<8, VT>(X, N, W, nb, dout, bias, Y, s);
+    else {
+        const int groups = (dout + kGroup - 1) / kGroup;
+        const int64_t grid = ((N + 63) / 64 * groups + 3) / 4;
+        if (grid > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
+        hipLaunchKernelGGL((linear_long_kernel<VT>), dim3((unsigned)grid), dim3(256), 0, s, X, N, W, nb, dout, groups, bias, Y);
+    }
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
 }
 
 }  // namespace
@@ -23,16 +260,9 @@ __global__ void linear_kernel(MxMatrix X, int64_t N, MxMatrix W, int din, int do
 maxk_status launch_mx_linear(const MxMatrix& X, int64_t N, const MxMatrix& W, int din, int dout, const float* bias, void* Y, int value_type,
                              hipStream_t s)
 {
-    const int64_t grid = (N * dout + 255) / 256;
-    if (grid > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
-#define MAXK_LINEAR(VT) \
-    hipLaunchKernelGGL((linear_kernel<VT>), dim3((unsigned)grid), dim3(256), 0, s, X, N, W, din, dout, bias, (value_store_t<VT>*)Y)
-    if (value_type == MAXK_VALUE_F32) MAXK_LINEAR(MAXK_VALUE_F32);
-    else if (value_type == MAXK_VALUE_BF16) MAXK_LINEAR(MAXK_VALUE_BF16);
-    else MAXK_LINEAR(MAXK_VALUE_F16);
-#undef MAXK_LINEAR
-    MAXK_LAUNCH_CHECK();
-    return MAXK_OK;
+    if (value_type == MAXK_VALUE_F32) return launch<MAXK_VALUE_F32>(X, N, W, din, dout, bias, (float*)Y, s);
+    if (value_type == MAXK_VALUE_BF16) return launch<MAXK_VALUE_BF16>(X, N, W, din, dout, bias, (uint16_t*)Y, s);
+    return launch<MAXK_VALUE_F16>(X, N, W, din, dout, bias, (uint16_t*)Y, s);
 }
 
 }  // namespace maxk
