@@ -5,7 +5,7 @@
 // over the rows of X, 16 at a time; the next 16 are on their way meanwhile.  Wavefronts that share rows of X lie in one workgroup, so X is read through L1.
 #include <algorithm>
 
-#include "mx.hpp"
+#include "mx_parts.hpp"
 
 namespace maxk {
 namespace {
@@ -69,13 +69,6 @@ __device__ __forceinline__ void load_blocks(Loaded<C>& x, const MxMatrix& A, int
     }
 }
 
-__device__ __forceinline__ void local_barrier()  // orders LDS only: loads and stores of memory stay under way
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 constexpr int kMaxGroups = 6;     // of a workgroup: up to 384 columns of Y
 constexpr int kPad = 4;           // floats at the end of a row in LDS, so that rows begin in different banks
 
@@ -134,7 +127,7 @@ __global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
             *reinterpret_cast<f32x4*>(room + (below + r) * pitch + wave % gcols * kGroup + t * 16 + g * 4) = products(w[t], x, start[t]);
-        local_barrier();  // the room of the step before was read before the one barrier, and is written after the next
+        local_fence();  // the room of the step before was read before the one barrier, and is written after the next
     };
     const auto whole_step = [&]() {
         make();
