@@ -6,6 +6,7 @@
 namespace maxk {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ void local_fence()  // orders LDS only: loads and stores of memory stay under way

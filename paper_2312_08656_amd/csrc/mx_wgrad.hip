@@ -8,6 +8,7 @@
 // turn, each with its own tiles of X and dH in LDS, and adds the groups' sums up in LDS at the end.  With two groups one fills its tiles while the other
 // multiplies.  The ranges' sums go to the workspace and a second kernel adds them up, always in the same order.
 #include <algorithm>
+#include <type_traits>
 
 #include "mx_parts.hpp"
 
@@ -20,18 +21,22 @@ constexpr int kStep = 32;  // rows
 template <int GR_, int WO_, int WI_, int WIT_>
 struct Shape {
     static constexpr int GR = GR_, WO = WO_, WI = WI_, WIT = WIT_;
-    static constexpr int TO = 64 * WO, TI = 32 * WIT * WI, WAVES = WO * WI, THREADS = 64 * GR * WAVES;
-    static constexpr int ACC = 2 * WIT * 16;               // accumulators a lane
-    static constexpr int TILE = WAVES * 64 * ACC;          // outputs
-    static constexpr int KGW = 4 / WAVES;                  // of the four runs of 8 rows of a step: those whose dH a wavefront brings
-    static constexpr int XITEMS = TI / 4 * 8 / (64 * WAVES);  // pieces of 4 columns x 4 rows of X a thread brings
+    static constexpr int TO = 64 * WO, TI = 32 * WIT * WI, WAVES = WO * WI, LANES = 64 * WAVES, THREADS = GR * LANES;
+    static constexpr int ACC = 2 * WIT * 16;                // accumulators a lane
+    static constexpr int TILE = LANES * ACC;                // outputs
+    static constexpr int KGW = 4 / WAVES;                   // of the four runs of 8 rows of a step: those whose CBSR entries a wavefront brings
+    static constexpr int XITEMS = TI / 16 * kStep / LANES;  // pieces of 16 columns of a row of X that a lane brings
 };
 using Small = Shape<8, 1, 1, 2>;   // 64 x 64: a wavefront a group
 using Middle = Shape<2, 2, 2, 2>;  // 128 x 128
 using Wide = Shape<2, 4, 1, 4>;    // 256 x 128
 
-enum Kind { kCbsr, kF32, kBf16, kF16 };
-__host__ __device__ constexpr int parts_of(int kind) { return kind == kBf16 ? 1 : kind == kF16 ? 2 : 3; }
+// How dH comes: CBSR by the bytes of a column, dense in 16-byte pieces (V) or element by element
+enum Kind { kCbsr1, kCbsr2, kCbsr4, kF32, kF32V, kBf16, kBf16V, kF16, kF16V };
+template <int KIND> using column_t = std::conditional_t<KIND == kCbsr1, uint8_t, std::conditional_t<KIND == kCbsr2, uint16_t, uint32_t>>;
+__host__ __device__ constexpr int type_of(int kind) { return kind <= kF32V ? MAXK_VALUE_F32 : kind <= kBf16V ? MAXK_VALUE_BF16 : MAXK_VALUE_F16; }
+__host__ __device__ constexpr int parts_of(int kind) { return kind <= kF32V ? 3 : kind <= kBf16V ? 1 : 2; }
+__host__ __device__ constexpr int piece_of(int kind) { return kind == kF32V ? 4 : kind == kBf16V || kind == kF16V ? 8 : 1; }  // columns
 
 struct Args {
     const uint8_t* codes;
@@ -47,17 +52,34 @@ struct Args {
     float* db;
 };
 
+// Tiles lie in LDS as the rows come, bf16, and are read transposed: a lane's operand is 8 rows of one column, and ds_read_b64_tr_b16 gives
+// 16 lanes 4 rows of 16 columns from 32 bytes of each of the rows.  The four rows of a read fall on different banks by the place of their bytes:
+// rows are multiples of 128 bytes, byte b of row r lies at b ^ 32 (r % 4).
+__device__ __forceinline__ int at_byte(int row, int byte, int pitch) { return row * pitch + (byte ^ (row & 3) << 5); }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ s16x4 read_transposed(const uint8_t* p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+}
+
 constexpr int kEntries = 4;  // entries of a run of 8 CBSR rows that a lane has under way (k <= 32: all of them)
 
 template <class S, int FMT, int KIND>
 __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
 {
-    constexpr int P = parts_of(KIND), XBYTES = S::TI * 64, DPART = S::TO * 64, GROUP = XBYTES + P * DPART;
-    constexpr int LOOP = S::GR * GROUP, JOIN = S::GR / 2 * S::TILE * 4, DBS = S::GR * S::TO * 4;
-    __shared__ __align__(16) uint8_t lds[(LOOP > JOIN ? LOOP : JOIN) > DBS ? (LOOP > JOIN ? LOOP : JOIN) : DBS];
+    constexpr bool CBSR = KIND <= kCbsr4;
+    constexpr int P = parts_of(KIND), VT = type_of(KIND), V = piece_of(KIND);
+    constexpr int XPITCH = S::TI * 2, DPITCH = S::TO * 2, XBYTES = kStep * XPITCH, DPART = kStep * DPITCH, GROUP = XBYTES + P * DPART;
+    constexpr int LOOP = S::GR * GROUP, JOIN = S::GR / 2 * S::TILE * 4;
+    // db: sums of a lane's operands, or of its columns over the rows that it brings; a copy each for what no lane adds up
+    constexpr int PIECES = S::TO / V, DITEMS = CBSR ? 1 : PIECES * kStep / S::LANES, COPIES = S::GR * (CBSR ? 1 : S::LANES / PIECES);
+    static_assert(CBSR || S::LANES % PIECES == 0);  // a lane's columns are the same in every row
+    constexpr int DBS = COPIES * S::TO * 4, ROOM = LOOP > JOIN ? LOOP : JOIN, LDS = ROOM > DBS ? ROOM : DBS;
+    __shared__ __align__(16) uint8_t lds[LDS];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / S::WAVES, w = wave % S::WAVES;
-    const int wo = w % S::WO, wi = w / S::WO;
+    const int wo = w % S::WO, wi = w / S::WO, me = w * 64 + lane;
     // a range's tiles run on one XCD, whose L2 holds the rows that they share
     const int tiles = A.otiles * A.itiles, at = blockIdx.x / 8, xcd = blockIdx.x % 8;
     const int tile = at % tiles;
@@ -68,83 +90,71 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     const int rounds = (int)((last - first + S::GR - 1) / S::GR);
     uint8_t* const xtile = lds + group * GROUP;
     uint8_t* const dtile = xtile + XBYTES;
+    const bool sums_db = A.dbsums && i0 == 0;
+    float* const dbcopies = reinterpret_cast<float*>(lds);
 
-    // what this thread brings of X: 4 columns of 4 rows; their places in LDS are [8 rows][column][row], columns 4c + j at j * TI / 4 + c
-    const int xrow_bytes = A.nb * (FMT == MAXK_MX_8 ? 32 : 16);
-    int xrow[S::XITEMS], xcol[S::XITEMS], xput[S::XITEMS], xblock[S::XITEMS];
-#pragma unroll
-    for (int n = 0; n < S::XITEMS; ++n) {
-        const int item = w * 64 + lane + n * 64 * S::WAVES, half = item & 1, c = (item >> 1) % (S::TI / 4), run = (item >> 1) / (S::TI / 4);
-        const int col = min(i0 + 4 * c, A.nb * kMxBlock - 4);
-        xrow[n] = run * 8 + half * 4;
-        xcol[n] = FMT == MAXK_MX_8 ? col : col / 2;
-        xblock[n] = col / kMxBlock;
-        xput[n] = (run * S::TI + c) * 16 + half * 8;
-    }
-    // and of dH: runs of 8 rows, whole
+    // what this lane brings of X: 16 columns of a row
+    constexpr int XWORDS = FMT == MAXK_MX_8 ? 4 : 2, XROW = S::TI / 16;
+    const int xrow_bytes = A.nb * (FMT == MAXK_MX_8 ? 32 : 16), xcol = min(i0 + me % XROW * 16, A.nb * kMxBlock - 16);
+    uint32_t xcode[S::XITEMS][XWORDS], xscale[S::XITEMS];
     int erow[kEntries];  // CBSR: row of the lane's entries in a run
-    if constexpr (KIND == kCbsr) {
+    if constexpr (CBSR) {
 #pragma unroll
         for (int e = 0; e < kEntries; ++e) erow[e] = (lane + 64 * e) / A.G.k;
     }
-
-    uint32_t xcode[S::XITEMS][4], xscale[S::XITEMS][4];
-    constexpr int VALS = KIND == kCbsr ? kEntries : S::TO / 64 * 8;
+    constexpr int VALS = CBSR ? kEntries : DITEMS * (V == 1 ? 1 : 4);
     float val[S::KGW][VALS];
-    uint32_t idx[S::KGW][KIND == kCbsr ? kEntries : 1];
+    uint32_t idx[S::KGW][CBSR ? kEntries : 1];
+    float dbsum[CBSR ? 2 : V];  // CBSR: of the two blocks' column that is the lane's
+#pragma unroll
+    for (int j = 0; j < (CBSR ? 2 : V); ++j) dbsum[j] = 0.f;
 
-    const auto index_at = [&](int64_t p) -> uint32_t {
-        return A.G.index_bytes == 1 ? ((const uint8_t*)A.G.sp_index)[p] : A.G.index_bytes == 2 ? ((const uint16_t*)A.G.sp_index)[p] : ((const uint32_t*)A.G.sp_index)[p];
-    };
     const auto load = [&](int round) {
         const int64_t row0 = min((first + (int64_t)round * S::GR + group) * kStep, A.N - 1);
         const int lim = (int)min(A.N - 1 - row0, (int64_t)kStep - 1);  // the last row that is there; rows past it are read from it, and are multiplied by 0
         const uint8_t* codes = A.codes + row0 * xrow_bytes;
         const uint8_t* scales = A.scales + row0 * A.nb;
 #pragma unroll
-        for (int n = 0; n < S::XITEMS; ++n)
+        for (int n = 0; n < S::XITEMS; ++n) {
+            const int row = min(me / XROW + n * (S::LANES / XROW), lim);
+            const uint8_t* p = codes + (uint32_t)(row * xrow_bytes + (FMT == MAXK_MX_8 ? xcol : xcol / 2));
+            if constexpr (FMT == MAXK_MX_8) *reinterpret_cast<uint4*>(xcode[n]) = *reinterpret_cast<const uint4*>(p);
+            else *reinterpret_cast<uint2*>(xcode[n]) = *reinterpret_cast<const uint2*>(p);
+            xscale[n] = scales[(uint32_t)(row * A.nb + xcol / kMxBlock)];
+        }
+        if constexpr (CBSR) {
+            const float* v = (const float*)A.G.values + row0 * A.G.k;
+            const column_t<KIND>* columns = (const column_t<KIND>*)A.G.sp_index + row0 * A.G.k;
+            const int end = (lim + 1) * A.G.k - 1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = min(xrow[n] + j, lim);
-                const uint8_t* p = codes + (uint32_t)(row * xrow_bytes + xcol[n]);
-                xcode[n][j] = FMT == MAXK_MX_8 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
-                xscale[n][j] = scales[(uint32_t)(row * A.nb + xblock[n])];
-            }
-#pragma unroll
-        for (int q = 0; q < S::KGW; ++q) {
-            const int run = w * S::KGW + q;
-            if constexpr (KIND == kCbsr) {
-                const float* v = (const float*)A.G.values + row0 * A.G.k;
-                const int end = (lim + 1) * A.G.k - 1;
+            for (int q = 0; q < S::KGW; ++q)
 #pragma unroll
                 for (int e = 0; e < kEntries; ++e) {
-                    const int p = min(run * 8 * A.G.k + lane + 64 * e, end);
-                    val[q][e] = v[(uint32_t)p];
-                    idx[q][e] = index_at(row0 * A.G.k + p);
+                    const uint32_t p = (uint32_t)min((w * S::KGW + q) * 8 * A.G.k + lane + 64 * e, end);
+                    val[q][e] = v[p];
+                    idx[q][e] = columns[p];
                 }
-            } else {
+        } else {
+            const value_store_t<VT>* values = (const value_store_t<VT>*)A.G.values + row0 * A.dout;
 #pragma unroll
-                for (int c = 0; c < S::TO / 64; ++c) {
-                    const int o = min(o0 + c * 64 + lane, A.dout - 1);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int64_t p = row0 * A.dout + (uint32_t)(min(run * 8 + j, lim) * A.dout + o);
-                        if constexpr (KIND == kF32) val[q][c * 8 + j] = ((const float*)A.G.values)[p];
-                        else val[q][c * 8 + j] = __uint_as_float(((const uint16_t*)A.G.values)[p]);  // widened when it is used
-                    }
-                }
+            for (int n = 0; n < DITEMS; ++n) {
+                const int item = me + n * S::LANES;
+                const uint32_t p = (uint32_t)(min(item / PIECES, lim) * A.dout + min(o0 + item % PIECES * V, A.dout - V));
+                if constexpr (V > 1) *reinterpret_cast<f32x4*>(&val[0][n * 4]) = *reinterpret_cast<const f32x4*>(values + p);
+                else if constexpr (VT == MAXK_VALUE_F32) val[0][n] = values[p];
+                else val[0][n] = __uint_as_float(values[p]);  // widened when it is used
             }
         }
     };
 
-    const auto put_entry = [&](int run, int row, uint32_t column, float x, int rows) {
+    const auto put_entry = [&](int row, uint32_t column, float x) {
         const uint32_t o = column - (uint32_t)o0;
-        if (row < 8 && run * 8 + row < rows && o < (uint32_t)S::TO) {
+        if (o < (uint32_t)S::TO) {
             float part[3];
             split<P>(x, part);
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                *reinterpret_cast<uint16_t*>(dtile + p * DPART + (run * S::TO + o) * 16 + row * 2) = (uint16_t)(__float_as_uint(part[p]) >> 16);
+                *reinterpret_cast<uint16_t*>(dtile + p * DPART + at_byte(row, (int)o * 2, DPITCH)) = (uint16_t)(__float_as_uint(part[p]) >> 16);
         }
     };
     const auto fill = [&](int round) {
@@ -152,56 +162,84 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         const int rows = (int)max((int64_t)0, min(min(last * kStep, A.N) - row0, (int64_t)kStep));
 #pragma unroll
         for (int n = 0; n < S::XITEMS; ++n) {
-            float x[4][4];  // [row][column]
+            uint32_t x[8];
+            if constexpr (FMT == MAXK_MX_8) {
+                const float unit = mx8_unit(xscale[n]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (FMT == MAXK_MX_8) {
-                    const float unit = mx8_unit(xscale[n][j]);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[j][c] = (float)(int8_t)(xcode[n][j] >> (8 * c)) * unit;
-                } else {
-                    const float scale = mx_scale(xscale[n][j]);
-                    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(xcode[n][j], scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(xcode[n][j], scale, 1);
-                    x[j][0] = a[0], x[j][1] = a[1], x[j][2] = b[0], x[j][3] = b[1];
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                *reinterpret_cast<uint2*>(xtile + xput[n] + c * (S::TI / 4) * 16) = make_uint2(uppers(x[0][c], x[1][c]), uppers(x[2][c], x[3][c]));
-        }
-#pragma unroll
-        for (int q = 0; q < S::KGW; ++q) {
-            const int run = w * S::KGW + q;
-            if constexpr (KIND == kCbsr) {
-                // a run's zeros and its entries come from one wavefront, whose LDS operations stay in order
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int c = 0; c < S::TO / 64; ++c)
-                        *reinterpret_cast<uint4*>(dtile + p * DPART + (run * S::TO + c * 64 + lane) * 16) = make_uint4(0, 0, 0, 0);
-                wave_fence();
-#pragma unroll
-                for (int e = 0; e < kEntries; ++e) put_entry(run, erow[e], idx[q][e], val[q][e], rows);
-                const int here = min(8, rows - run * 8) * A.G.k;
-                for (int e = lane + 64 * kEntries; e < here; e += 64) {  // k above 32
-                    const int64_t p = (row0 + run * 8) * A.G.k + e;
-                    put_entry(run, e / A.G.k, index_at(p), ((const float*)A.G.values)[p], rows);
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t c = xcode[n][j / 2] >> (16 * (j & 1));
+                    x[j] = uppers((float)(int8_t)c * unit, (float)(int8_t)(c >> 8) * unit);
                 }
             } else {
+                const float scale = mx_scale(xscale[n]);
 #pragma unroll
-                for (int c = 0; c < S::TO / 64; ++c) {
-                    float part[8][3];
+                for (int j = 0; j < 2; ++j) {
+                    x[4 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(xcode[n][j], scale, 0));
+                    x[4 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(xcode[n][j], scale, 1));
+                    x[4 * j + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(xcode[n][j], scale, 2));
+                    x[4 * j + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(xcode[n][j], scale, 3));
+                }
+            }
+            uint4* to = reinterpret_cast<uint4*>(xtile + at_byte(me / XROW + n * (S::LANES / XROW), me % XROW * 32, XPITCH));
+            to[0] = make_uint4(x[0], x[1], x[2], x[3]);
+            to[1] = make_uint4(x[4], x[5], x[6], x[7]);
+        }
+        if constexpr (CBSR) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float x = val[q][c * 8 + j];
-                        if constexpr (KIND == kBf16) x = widen_value<MAXK_VALUE_BF16>((uint16_t)__float_as_uint(x));
-                        if constexpr (KIND == kF16) x = widen_value<MAXK_VALUE_F16>((uint16_t)__float_as_uint(x));
-                        split<P>(run * 8 + j < rows ? x : 0.f, part[j]);
-                    }
+            for (int q = 0; q < S::KGW; ++q) {
+                const int run = w * S::KGW + q;
+                if constexpr (S::WI > 1) {  // a run's zeros and its entries come from one wavefront, whose LDS operations stay in order
 #pragma unroll
                     for (int p = 0; p < P; ++p)
-                        *reinterpret_cast<uint4*>(dtile + p * DPART + (run * S::TO + c * 64 + lane) * 16) =
-                            make_uint4(uppers(part[0][p], part[1][p]), uppers(part[2][p], part[3][p]), uppers(part[4][p], part[5][p]), uppers(part[6][p], part[7][p]));
+#pragma unroll
+                        for (int c = 0; c < S::TO / 64; ++c) *reinterpret_cast<uint4*>(dtile + p * DPART + run * 8 * DPITCH + (c * 64 + lane) * 16) = make_uint4(0, 0, 0, 0);
+                    wave_fence();
+                }
+                const int there = min(8, rows - run * 8);
+#pragma unroll
+                for (int e = 0; e < kEntries; ++e)
+                    if (erow[e] < there) put_entry(run * 8 + erow[e], idx[q][e], val[q][e]);
+                for (int e = lane + 64 * kEntries; e < there * A.G.k; e += 64) {  // k above 32
+                    const int64_t p = (row0 + run * 8) * A.G.k + e;
+                    put_entry(run * 8 + e / A.G.k, ((const column_t<KIND>*)A.G.sp_index)[p], ((const float*)A.G.values)[p]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < DITEMS; ++n) {
+                const int item = me + n * S::LANES, row = item / PIECES, byte = item % PIECES * V * 2;
+                uint8_t* to = dtile + at_byte(row, byte, DPITCH);
+                const bool there = row < rows;
+                if constexpr (KIND == kBf16V) {  // as it is
+                    uint4 u = __builtin_bit_cast(uint4, *reinterpret_cast<const f32x4*>(&val[0][n * 4]));
+                    if (!there) u = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(to) = u;
+                    const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        dbsum[2 * j] += __uint_as_float(word[j] << 16);
+                        dbsum[2 * j + 1] += __uint_as_float(word[j] & 0xFFFF0000u);
+                    }
+                } else {
+                    float part[V][3];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        float x;
+                        if constexpr (KIND == kF16V) x = widen_value<VT>((uint16_t)(__float_as_uint(val[0][n * 4 + j / 2]) >> (16 * (j & 1))));
+                        else if constexpr (VT == MAXK_VALUE_F32) x = val[0][n * (V == 1 ? 1 : 4) + j];
+                        else x = widen_value<VT>((uint16_t)__float_as_uint(val[0][n]));
+                        x = there ? x : 0.f;
+                        dbsum[j] += x;
+                        split<P>(x, part[j]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        if constexpr (V == 8)
+                            *reinterpret_cast<uint4*>(to + p * DPART) = make_uint4(uppers(part[0][p], part[1][p]), uppers(part[2][p], part[3][p]),
+                                                                                   uppers(part[4][p], part[5][p]), uppers(part[6][p], part[7][p]));
+                        else if constexpr (V == 4) *reinterpret_cast<uint2*>(to + p * DPART) = make_uint2(uppers(part[0][p], part[1][p]), uppers(part[2][p], part[3][p]));
+                        else *reinterpret_cast<uint16_t*>(to + p * DPART) = (uint16_t)(__float_as_uint(part[0][p]) >> 16);
+                    }
                 }
             }
         }
@@ -214,27 +252,51 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         for (int b = 0; b < S::WIT; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[a][b][r] = 0.f;
-    const bool sums_db = A.dbsums && i0 == 0 && wi == 0;
-    float dbsum[2] = {0.f, 0.f};
+    // where a lane's part of an operand begins, for an even and an odd block of 32 columns
+    const int trow = (lane >> 5) * 8 + (lane & 15) / 4, tbyte = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+    const auto operand = [&](const uint8_t* base, int pitch, int block, int half) {
+        const uint8_t* p = base + at_byte(trow, tbyte + (block & 1) * 64, pitch) + block / 2 * 128 + half * 16 * pitch;
+        const s16x4 low = read_transposed(p), high = read_transposed(p + 4 * pitch);
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // CBSR: the tile of dH is zeros between the steps.  Where one wavefront alone reads its 64 columns, it clears them as it goes, so that
+    // the clearing is spread over the products and does not hold up the other group's first reads.
+    constexpr bool CLEARS = CBSR && S::WI == 1;
+    const auto clear_d = [&](int p, int half) {
+        uint8_t* to = dtile + p * DPART + (half * 16 + lane / 8) * DPITCH + wo * 128 + lane % 8 * 16;
+        *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(to + 8 * DPITCH) = make_uint4(0, 0, 0, 0);
+    };
     const auto multiply = [&]() {
+        // 2 halves of 16 rows x P parts (the smallest first) x 2 blocks of 32 columns of dH, each with all blocks of X; operands are read
+        // AHEAD products before they are needed, the second half's of X meanwhile
+        constexpr int STEPS = 4 * P, AHEAD = 2;
+        bf16x8 x[2][S::WIT], d[AHEAD + 1];
+        const auto fetch_x = [&](int half, int b) { x[half][b] = operand(xtile + wi * S::WIT * 64, XPITCH, b, half); };
+        const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART + wo * 128, DPITCH, t % 2, t / (2 * P)); };
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int run = 2 * h + (lane >> 5), l = lane & 31;
-            bf16x8 x[S::WIT];
+        for (int b = 0; b < S::WIT; ++b) fetch_x(0, b);
 #pragma unroll
-            for (int b = 0; b < S::WIT; ++b) x[b] = *reinterpret_cast<const bf16x8*>(xtile + (run * S::TI + (wi * S::WIT + b) * 32 + l) * 16);
+        for (int t = 0; t < AHEAD; ++t) fetch_d(t);
 #pragma unroll
-            for (int p = P - 1; p >= 0; --p)  // the smallest first
+        for (int t = 0; t < STEPS; ++t) {
+            if (t + AHEAD < STEPS) fetch_d(t + AHEAD);
+            if (CLEARS && t % 2 == 1) clear_d(P - 1 - t % (2 * P) / 2, t / (2 * P));  // both blocks have been read
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    const bf16x8 d = *reinterpret_cast<const bf16x8*>(dtile + p * DPART + (run * S::TO + wo * 64 + a * 32 + l) * 16);
+            for (int b = 0; b < S::WIT; ++b)
+                if (t < 2 * P && b * 2 * P / S::WIT == t) fetch_x(1, b);
 #pragma unroll
-                    for (int b = 0; b < S::WIT; ++b) sum[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d, x[b], sum[a][b], 0, 0, 0);
-                    if (sums_db) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) dbsum[a] += (float)d[j];
-                    }
-                }
+            for (int b = 0; b < S::WIT; ++b)
+                sum[t % 2][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[t % (AHEAD + 1)], x[t / (2 * P)][b], sum[t % 2][b], 0, 0, 0);
+            if constexpr (CBSR) {  // db while the products run
+                const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+                const bf16x8& y = d[t % (AHEAD + 1)];
+                float even = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 0, 1), one, dbsum[t % 2], false);
+                even = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 2, 3), one, even, false);
+                even = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 4, 5), one, even, false);
+                dbsum[t % 2] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 6, 7), one, even, false);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     const auto sync = [&]() {
@@ -243,14 +305,23 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     };
 
     load(0);
+    if constexpr (CLEARS) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) clear_d(p, half);
+        sync();
+    }
     if constexpr (S::WAVES > 1) {
         if (group & 1) local_fence();  // half a round behind the other group
     }
     for (int round = 0; round < rounds; ++round) {
         fill(round);
         sync();
+        __builtin_amdgcn_s_setprio(3);  // products first: the other group's stores to LDS can wait, the operands cannot
         load(round + 1);
         multiply();
+        __builtin_amdgcn_s_setprio(0);
         sync();
     }
     if constexpr (S::WAVES > 1) {
@@ -283,18 +354,22 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         local_fence();
     }
     if (sums_db) {
+        if constexpr (CBSR) {
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const float s = dbsum[a] + __shfl_xor(dbsum[a], 32);
-            if (lane < 32) room[group * S::TO + wo * 64 + a * 32 + lane] = s;
+            for (int a = 0; a < 2; ++a) {
+                const float both = dbsum[a] + __shfl_xor(dbsum[a], 32);  // the lanes' rows
+                if (wi == 0 && lane < 32) dbcopies[group * S::TO + wo * 64 + a * 32 + lane] = both;
+            }
+        } else {
+            float* mine = dbcopies + (group * (COPIES / S::GR) + me / PIECES) * S::TO + me % PIECES * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) mine[j] = dbsum[j];
         }
-    }
-    local_fence();
-    if (A.dbsums && i0 == 0) {
+        local_fence();
         for (int o = threadIdx.x; o < S::TO; o += S::THREADS) {
             float s = 0.f;
 #pragma unroll
-            for (int g = 0; g < S::GR; ++g) s += room[g * S::TO + o];
+            for (int g = 0; g < COPIES; ++g) s += dbcopies[g * S::TO + o];
             if (A.ranges > 1) A.dbsums[range * A.otiles * S::TO + o0 + o] = s;
             else if (o0 + o < A.dout) A.db[o0 + o] = s;
         }
@@ -313,7 +388,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int b = 0; b < S::WIT; ++b) {
-                const int p = (wi * S::WIT + b) * 32 + (lane & 31), i = i0 + p % (S::TI / 4) * 4 + p / (S::TI / 4);
+                const int i = i0 + (wi * S::WIT + b) * 32 + (lane & 31);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int o = o0 + wo * 64 + a * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
@@ -347,7 +422,7 @@ __global__ void __launch_bounds__(256) add_ranges_kernel(const Args A)
     }
     const int tile = (int)(at / S::TILE), in = (int)(at % S::TILE), w = in / (64 * S::ACC), reg = in / 64 % S::ACC;
     const int wo = w % S::WO, wi = w / S::WO, a = reg / (16 * S::WIT), b = reg / 16 % S::WIT, r = reg % 16;
-    const int pos = (wi * S::WIT + b) * 32 + (lane & 31), i = tile % A.itiles * S::TI + pos % (S::TI / 4) * 4 + pos / (S::TI / 4);
+    const int i = tile % A.itiles * S::TI + (wi * S::WIT + b) * 32 + (lane & 31);
     const int o = tile / A.itiles * S::TO + wo * 64 + a * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
     if (o < A.dout && i < A.din) A.dW[(int64_t)o * A.din + i] = s;
 }
@@ -395,11 +470,21 @@ template <class S>
 maxk_status run_shape(const Args& A, int format, hipStream_t s)
 {
     maxk_status st;
+    const bool pieces = aligned(A.G.values, 16) && A.dout * (A.G.value_type == MAXK_VALUE_F32 ? 4 : 2) % 16 == 0;  // rows of whole 16-byte pieces
 #define MAXK_KIND(KIND) st = format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND>(A, s) : run<S, MAXK_MX_4, KIND>(A, s)
-    if (A.G.k) MAXK_KIND(kCbsr);
-    else if (A.G.value_type == MAXK_VALUE_F32) MAXK_KIND(kF32);
-    else if (A.G.value_type == MAXK_VALUE_BF16) MAXK_KIND(kBf16);
-    else MAXK_KIND(kF16);
+    if (A.G.k && A.G.index_bytes == 1) MAXK_KIND(kCbsr1);
+    else if (A.G.k && A.G.index_bytes == 2) MAXK_KIND(kCbsr2);
+    else if (A.G.k) MAXK_KIND(kCbsr4);
+    else if (A.G.value_type == MAXK_VALUE_F32) {
+        if (pieces) MAXK_KIND(kF32V);
+        else MAXK_KIND(kF32);
+    } else if (A.G.value_type == MAXK_VALUE_BF16) {
+        if (pieces) MAXK_KIND(kBf16V);
+        else MAXK_KIND(kBf16);
+    } else {
+        if (pieces) MAXK_KIND(kF16V);
+        else MAXK_KIND(kF16);
+    }
 #undef MAXK_KIND
     if (st != MAXK_OK || A.ranges == 1) return st;
     const int64_t outputs = (int64_t)A.otiles * A.itiles * S::TILE + (A.dbsums ? (int64_t)A.otiles * S::TO : 0);
