@@ -29,7 +29,6 @@ __host__ __device__ constexpr int parts_of(int kind) { return kind <= kF32V ? 3 
 
 template <int KIND> using column_t = std::conditional_t<KIND == kCbsr1, uint8_t, std::conditional_t<KIND == kCbsr2, uint16_t, uint32_t>>;
 
-constexpr int kEntries = 4;  // CBSR entries of its rows that a lane has under way
 
 struct Args {
     MxGrad G;
@@ -43,7 +42,8 @@ struct Args {
 };
 
 // CHUNKED: dH is wider than a tile, which takes it in chunks (W comes anew with each)
-template <class S, int KIND, bool CHUNKED>
+// E: CBSR entries of its rows that a lane has under way; those of wider rows come in turns
+template <class S, int KIND, int E, bool CHUNKED>
 __global__ void __launch_bounds__(S::THREADS) input_grad_kernel(const Args A)
 {
     constexpr int P = parts_of(KIND), VT = type_of(KIND), PART = kRows * S::KC * 32, TILE = P * PART;
@@ -89,21 +89,21 @@ __global__ void __launch_bounds__(S::THREADS) input_grad_kernel(const Args A)
     };
 
     const int k = A.G.k;
-    int erow[kEntries];
+    int erow[E];
     if constexpr (KIND <= kCbsr4) {
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) erow[e] = (lane + 64 * e) / k;
+        for (int e = 0; e < E; ++e) erow[e] = (lane + 64 * e) / k;
     }
-    constexpr int VALS = KIND <= kCbsr4 ? kEntries : VT == MAXK_VALUE_F32 || KIND == kBf16 || KIND == kF16 ? S::UNITS * 8 : S::UNITS * 4;
+    constexpr int VALS = KIND <= kCbsr4 ? E : VT == MAXK_VALUE_F32 || KIND == kBf16 || KIND == kF16 ? S::UNITS * 8 : S::UNITS * 4;
     float val[VALS];  // 16-byte pieces of 16-bit values: two to a register
-    uint32_t idx[KIND <= kCbsr4 ? kEntries : 1];
+    uint32_t idx[KIND <= kCbsr4 ? E : 1];
     const auto load = [&](int64_t t, int chunk) {
         const int64_t row0 = min(t, tiles - 1) * kRows;
         const int lim = (int)min(A.N - 1 - row0, (int64_t)kRows - 1);  // rows past the last one are read from it; what they give is not stored
         if constexpr (KIND <= kCbsr4) {
             const int end = (lim + 1) * k - 1;
 #pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
+            for (int e = 0; e < E; ++e) {
                 const uint32_t p = (uint32_t)min(w * S::ROWS * k + lane + 64 * e, end);
                 val[e] = ((const float*)A.G.values + row0 * k)[p];
                 idx[e] = ((const column_t<KIND>*)A.G.sp_index + row0 * k)[p];
@@ -152,13 +152,21 @@ __global__ void __launch_bounds__(S::THREADS) input_grad_kernel(const Args A)
                 }
             };
 #pragma unroll
-            for (int e = 0; e < kEntries; ++e)
+            for (int e = 0; e < E; ++e)
                 if (erow[e] < S::ROWS) put(w * S::ROWS + erow[e], idx[e], val[e]);
             const int64_t row0 = min(t, tiles - 1) * kRows;
-            const int here = ((int)min(A.N - row0, (int64_t)kRows) - w * S::ROWS) * k;
-            for (int e = lane + 64 * kEntries; e < min(here, S::ROWS * k); e += 64) {
-                const int64_t p = (row0 + w * S::ROWS) * k + e;
-                put(w * S::ROWS + e / k, ((const column_t<KIND>*)A.G.sp_index)[p], ((const float*)A.G.values)[p]);
+            const int end = min(((int)min(A.N - row0, (int64_t)kRows) - w * S::ROWS) * k, S::ROWS * k) - 1;
+            for (int e0 = 64 * E; e0 <= end; e0 += 64 * E) {
+                const int64_t mine = (row0 + w * S::ROWS) * k;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const uint32_t p = (uint32_t)min(e0 + lane + 64 * e, end);
+                    val[e] = ((const float*)A.G.values + mine)[p];
+                    idx[e] = ((const column_t<KIND>*)A.G.sp_index + mine)[p];
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e0 + lane + 64 * e <= end) put(w * S::ROWS + (e0 + lane + 64 * e) / k, idx[e], val[e]);
             }
         } else {
 #pragma unroll
@@ -258,7 +266,7 @@ __global__ void __launch_bounds__(S::THREADS) input_grad_kernel(const Args A)
     if (S::GR > 1 && !(group & 1)) local_fence();
 }
 
-template <class S, int KIND, bool CHUNKED = false>
+template <class S, int KIND, int E, bool CHUNKED = false>
 maxk_status run(Args A, hipStream_t s)
 {
     A.spans = (A.din + S::SPAN - 1) / S::SPAN;
@@ -266,20 +274,20 @@ maxk_status run(Args A, hipStream_t s)
     const int64_t tiles = (A.N + kRows - 1) / kRows;
     A.slots = std::max<int64_t>(1, std::min((tiles + S::GR - 1) / S::GR, (int64_t)512 / A.spans));
     const int64_t grid = (A.slots + 7) / 8 * A.spans * 8;
-    hipLaunchKernelGGL((input_grad_kernel<S, KIND, CHUNKED>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
+    hipLaunchKernelGGL((input_grad_kernel<S, KIND, E, CHUNKED>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
 
-template <int KIND>
+template <int KIND, int E = 1>
 maxk_status run_kind(const Args& A, hipStream_t s)
 {
     const bool two = A.din > 128;  // columns of dX that four wavefronts hold, 32 each
-    if (A.dout <= 64) return two ? run<Shape<4, 2, 4, 2>, KIND>(A, s) : run<Shape<4, 1, 4, 2>, KIND>(A, s);
-    if (A.dout <= 128) return two ? run<Shape<8, 2, 4, 2>, KIND>(A, s) : run<Shape<8, 1, 4, 2>, KIND>(A, s);
-    if (A.dout <= 256) return two ? run<Shape<16, 2, 4, 2>, KIND>(A, s) : run<Shape<16, 1, 4, 2>, KIND>(A, s);
-    if (A.dout <= 512) return run<Shape<32, 1, 8, 1>, KIND>(A, s);
-    return run<Shape<16, 2, 4, 2>, KIND, true>(A, s);
+    if (A.dout <= 64) return two ? run<Shape<4, 2, 4, 2>, KIND, E>(A, s) : run<Shape<4, 1, 4, 2>, KIND, E>(A, s);
+    if (A.dout <= 128) return two ? run<Shape<8, 2, 4, 2>, KIND, E>(A, s) : run<Shape<8, 1, 4, 2>, KIND, E>(A, s);
+    if (A.dout <= 256) return two ? run<Shape<16, 2, 4, 2>, KIND, E>(A, s) : run<Shape<16, 1, 4, 2>, KIND, E>(A, s);
+    if (A.dout <= 512) return run<Shape<32, 1, 8, 1>, KIND, E>(A, s);
+    return run<Shape<16, 2, 4, 2>, KIND, E, true>(A, s);
 }
 
 }  // namespace
@@ -288,7 +296,9 @@ maxk_status launch_mx_input_grad(const MxGrad& G, int64_t N, const MxMatrix& W, 
 {
     const size_t xb = value_type == MAXK_VALUE_F32 ? 4 : 2, gb = G.value_type == MAXK_VALUE_F32 ? 4 : 2;
     const Args A = {G, N, W, din, dout, mx_blocks(din), 0, 0, 0, dX, value_type, din % 2 == 0 && aligned(dX, 2 * xb)};
-    if (G.k) return G.index_bytes == 1 ? run_kind<kCbsr1>(A, s) : G.index_bytes == 2 ? run_kind<kCbsr2>(A, s) : run_kind<kCbsr4>(A, s);
+#define MAXK_ENTRIES(KIND) (G.k <= 32 ? run_kind<KIND, 4>(A, s) : run_kind<KIND, 8>(A, s))
+    if (G.k) return G.index_bytes == 1 ? MAXK_ENTRIES(kCbsr1) : G.index_bytes == 2 ? MAXK_ENTRIES(kCbsr2) : MAXK_ENTRIES(kCbsr4);
+#undef MAXK_ENTRIES
     const bool pieces = dout * gb % 16 == 0 && aligned(G.values, 16);
     if (G.value_type == MAXK_VALUE_F32) return pieces ? run_kind<kF32V>(A, s) : run_kind<kF32>(A, s);
     if (G.value_type == MAXK_VALUE_BF16) return pieces ? run_kind<kBf16V>(A, s) : run_kind<kBf16>(A, s);

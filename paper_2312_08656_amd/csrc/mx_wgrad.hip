@@ -63,9 +63,8 @@ __device__ __forceinline__ s16x4 read_transposed(const uint8_t* p)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
-constexpr int kEntries = 4;  // entries of a run of 8 CBSR rows that a lane has under way (k <= 32: all of them)
-
-template <class S, int FMT, int KIND>
+// E: entries of a run of 8 CBSR rows that a lane has under way (k / 8, up to 16; those of wider rows come in turns)
+template <class S, int FMT, int KIND, int E>
 __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
 {
     constexpr bool CBSR = KIND <= kCbsr4;
@@ -97,14 +96,14 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     constexpr int XWORDS = FMT == MAXK_MX_8 ? 4 : 2, XROW = S::TI / 16;
     const int xrow_bytes = A.nb * (FMT == MAXK_MX_8 ? 32 : 16), xcol = min(i0 + me % XROW * 16, A.nb * kMxBlock - 16);
     uint32_t xcode[S::XITEMS][XWORDS], xscale[S::XITEMS];
-    int erow[kEntries];  // CBSR: row of the lane's entries in a run
+    int erow[E];  // CBSR: row of the lane's entries in a run
     if constexpr (CBSR) {
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) erow[e] = (lane + 64 * e) / A.G.k;
+        for (int e = 0; e < E; ++e) erow[e] = (lane + 64 * e) / A.G.k;
     }
-    constexpr int VALS = CBSR ? kEntries : DITEMS * (V == 1 ? 1 : 4);
+    constexpr int VALS = CBSR ? E : DITEMS * (V == 1 ? 1 : 4);
     float val[S::KGW][VALS];
-    uint32_t idx[S::KGW][CBSR ? kEntries : 1];
+    uint32_t idx[S::KGW][CBSR ? E : 1];
     float dbsum[CBSR ? 2 : V];  // CBSR: of the two blocks' column that is the lane's
 #pragma unroll
     for (int j = 0; j < (CBSR ? 2 : V); ++j) dbsum[j] = 0.f;
@@ -129,7 +128,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
 #pragma unroll
             for (int q = 0; q < S::KGW; ++q)
 #pragma unroll
-                for (int e = 0; e < kEntries; ++e) {
+                for (int e = 0; e < E; ++e) {
                     const uint32_t p = (uint32_t)min((w * S::KGW + q) * 8 * A.G.k + lane + 64 * e, end);
                     val[q][e] = v[p];
                     idx[q][e] = columns[p];
@@ -197,11 +196,20 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
                 }
                 const int there = min(8, rows - run * 8);
 #pragma unroll
-                for (int e = 0; e < kEntries; ++e)
+                for (int e = 0; e < E; ++e)
                     if (erow[e] < there) put_entry(run * 8 + erow[e], idx[q][e], val[q][e]);
-                for (int e = lane + 64 * kEntries; e < there * A.G.k; e += 64) {  // k above 32
-                    const int64_t p = (row0 + run * 8) * A.G.k + e;
-                    put_entry(run * 8 + e / A.G.k, ((const column_t<KIND>*)A.G.sp_index)[p], ((const float*)A.G.values)[p]);
+                for (int e0 = 64 * E; e0 < there * A.G.k; e0 += 64 * E) {
+                    const int64_t run0 = (row0 + run * 8) * A.G.k;
+                    const int end = there * A.G.k - 1;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const uint32_t p = (uint32_t)min(e0 + lane + 64 * e, end);
+                        val[q][e] = ((const float*)A.G.values + run0)[p];
+                        idx[q][e] = ((const column_t<KIND>*)A.G.sp_index + run0)[p];
+                    }
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e0 + lane + 64 * e <= end) put_entry(run * 8 + (e0 + lane + 64 * e) / A.G.k, idx[q][e], val[q][e]);
                 }
             }
         } else {
@@ -456,12 +464,12 @@ Plan plan(int64_t N, int din, int dout)
     return plan_of<Middle>(1, N, din, dout);
 }
 
-template <class S, int FMT, int KIND>
+template <class S, int FMT, int KIND, int E = 1>
 maxk_status run(const Args& A, hipStream_t s)
 {
     const int64_t tiles = (int64_t)A.otiles * A.itiles, grid = (A.ranges + 7) / 8 * tiles * 8;
     if (grid > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
-    hipLaunchKernelGGL((weight_grad_kernel<S, FMT, KIND>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
+    hipLaunchKernelGGL((weight_grad_kernel<S, FMT, KIND, E>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
@@ -470,11 +478,16 @@ template <class S>
 maxk_status run_shape(const Args& A, int format, hipStream_t s)
 {
     maxk_status st;
+    constexpr int WIDEST = S::TO == 128 ? 16 : 8;  // 64 columns of dH have k up to 64; 256 and 16 entries would not fit the registers
     const bool pieces = aligned(A.G.values, 16) && A.dout * (A.G.value_type == MAXK_VALUE_F32 ? 4 : 2) % 16 == 0;  // rows of whole 16-byte pieces
+#define MAXK_ENTRIES(KIND)                                                                                                                            \
+    st = A.G.k <= 32   ? (format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND, 4>(A, s) : run<S, MAXK_MX_4, KIND, 4>(A, s))                                  \
+         : A.G.k <= 64 ? (format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND, 8>(A, s) : run<S, MAXK_MX_4, KIND, 8>(A, s))                                  \
+                       : (format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND, WIDEST>(A, s) : run<S, MAXK_MX_4, KIND, WIDEST>(A, s))
 #define MAXK_KIND(KIND) st = format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND>(A, s) : run<S, MAXK_MX_4, KIND>(A, s)
-    if (A.G.k && A.G.index_bytes == 1) MAXK_KIND(kCbsr1);
-    else if (A.G.k && A.G.index_bytes == 2) MAXK_KIND(kCbsr2);
-    else if (A.G.k) MAXK_KIND(kCbsr4);
+    if (A.G.k && A.G.index_bytes == 1) MAXK_ENTRIES(kCbsr1);
+    else if (A.G.k && A.G.index_bytes == 2) MAXK_ENTRIES(kCbsr2);
+    else if (A.G.k) MAXK_ENTRIES(kCbsr4);
     else if (A.G.value_type == MAXK_VALUE_F32) {
         if (pieces) MAXK_KIND(kF32V);
         else MAXK_KIND(kF32);
@@ -486,6 +499,7 @@ maxk_status run_shape(const Args& A, int format, hipStream_t s)
         else MAXK_KIND(kF16);
     }
 #undef MAXK_KIND
+#undef MAXK_ENTRIES
     if (st != MAXK_OK || A.ranges == 1) return st;
     const int64_t outputs = (int64_t)A.otiles * A.itiles * S::TILE + (A.dbsums ? (int64_t)A.otiles * S::TO : 0);
     hipLaunchKernelGGL((add_ranges_kernel<S>), dim3((unsigned)(outputs / 64)), dim3(256), 0, s, A);
