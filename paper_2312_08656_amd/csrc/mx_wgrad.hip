@@ -31,13 +31,6 @@ using Small = Shape<8, 1, 1, 2>;   // 64 x 64: a wavefront a group
 using Middle = Shape<2, 2, 2, 2>;  // 128 x 128
 using Wide = Shape<2, 4, 1, 4>;    // 256 x 128
 
-// How dH comes: CBSR by the bytes of a column, dense in 16-byte pieces (V) or element by element
-enum Kind { kCbsr1, kCbsr2, kCbsr4, kF32, kF32V, kBf16, kBf16V, kF16, kF16V };
-template <int KIND> using column_t = std::conditional_t<KIND == kCbsr1, uint8_t, std::conditional_t<KIND == kCbsr2, uint16_t, uint32_t>>;
-__host__ __device__ constexpr int type_of(int kind) { return kind <= kF32V ? MAXK_VALUE_F32 : kind <= kBf16V ? MAXK_VALUE_BF16 : MAXK_VALUE_F16; }
-__host__ __device__ constexpr int parts_of(int kind) { return kind <= kF32V ? 3 : kind <= kBf16V ? 1 : 2; }
-__host__ __device__ constexpr int piece_of(int kind) { return kind == kF32V ? 4 : kind == kBf16V || kind == kF16V ? 8 : 1; }  // columns
-
 struct Args {
     const uint8_t* codes;
     const uint8_t* scales;
@@ -51,17 +44,6 @@ struct Args {
     float* dW;     // written at once where there is one range
     float* db;
 };
-
-// Tiles lie in LDS as the rows come, bf16, and are read transposed: a lane's operand is 8 rows of one column, and ds_read_b64_tr_b16 gives
-// 16 lanes 4 rows of 16 columns from 32 bytes of each of the rows.  The four rows of a read fall on different banks by the place of their bytes:
-// rows are multiples of 128 bytes, byte b of row r lies at b ^ 32 (r % 4).
-__device__ __forceinline__ int at_byte(int row, int byte, int pitch) { return row * pitch + (byte ^ (row & 3) << 5); }
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ s16x4 read_transposed(const uint8_t* p)
-{
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
-}
 
 // E: entries of a run of 8 CBSR rows that a lane has under way (k / 8, up to 16; those of wider rows come in turns)
 template <class S, int FMT, int KIND, int E>
@@ -260,13 +242,6 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         for (int b = 0; b < S::WIT; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[a][b][r] = 0.f;
-    // where a lane's part of an operand begins, for an even and an odd block of 32 columns
-    const int trow = (lane >> 5) * 8 + (lane & 15) / 4, tbyte = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-    const auto operand = [&](const uint8_t* base, int pitch, int block, int half) {
-        const uint8_t* p = base + at_byte(trow, tbyte + (block & 1) * 64, pitch) + block / 2 * 128 + half * 16 * pitch;
-        const s16x4 low = read_transposed(p), high = read_transposed(p + 4 * pitch);
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
     // CBSR: the tile of dH is zeros between the steps.  Where one wavefront alone reads its 64 columns, it clears them as it goes, so that
     // the clearing is spread over the products and does not hold up the other group's first reads.
     constexpr bool CLEARS = CBSR && S::WI == 1;
@@ -280,8 +255,8 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         // AHEAD products before they are needed, the second half's of X meanwhile
         constexpr int STEPS = 4 * P, AHEAD = 2;
         bf16x8 x[2][S::WIT], d[AHEAD + 1];
-        const auto fetch_x = [&](int half, int b) { x[half][b] = operand(xtile + wi * S::WIT * 64, XPITCH, b, half); };
-        const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART + wo * 128, DPITCH, t % 2, t / (2 * P)); };
+        const auto fetch_x = [&](int half, int b) { x[half][b] = transposed_operand(xtile + wi * S::WIT * 64, XPITCH, b, half * 16, lane); };
+        const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = transposed_operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART + wo * 128, DPITCH, t % 2, t / (2 * P) * 16, lane); };
 #pragma unroll
         for (int b = 0; b < S::WIT; ++b) fetch_x(0, b);
 #pragma unroll
