@@ -130,7 +130,8 @@ def _load_fast(lib: ctypes.CDLL) -> None:
         return
     _torch_calls.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.maxk_topk_cbsr_narrow, lib.maxk_spgemm_fwd_narrow, lib.maxk_spgemm_fwd_noalloc, lib.maxk_sspmm_bwd_narrow,
-        lib.maxk_cbsr_scatter)], _check)
+        lib.maxk_cbsr_scatter, lib.maxk_mx_quantize, lib.maxk_mx_dequantize, lib.maxk_mx_linear, lib.maxk_mx_weight_grad_workspace,
+        lib.maxk_mx_weight_grad, lib.maxk_mx_weight_grad_cbsr, lib.maxk_mx_input_grad, lib.maxk_mx_input_grad_cbsr)], _check)
     _FAST = _torch_calls
 
 

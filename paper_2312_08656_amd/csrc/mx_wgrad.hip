@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
                     *reinterpret_cast<uint4*>(to) = u;
                     const uint32_t word[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; sums_db && j < 4; ++j) {
                         dbsum[2 * j] += __uint_as_float(word[j] << 16);
                         dbsum[2 * j + 1] += __uint_as_float(word[j] & 0xFFFF0000u);
                     }
@@ -250,10 +250,11 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
         *reinterpret_cast<uint4*>(to + 8 * DPITCH) = make_uint4(0, 0, 0, 0);
     };
-    const auto multiply = [&]() {
+    // meanwhile: what else the wavefront has to do, once the first products are under way
+    const auto multiply = [&](auto meanwhile) {
         // 2 halves of 16 rows x P parts (the smallest first) x 2 blocks of 32 columns of dH, each with all blocks of X; operands are read
         // AHEAD products before they are needed, the second half's of X meanwhile
-        constexpr int STEPS = 4 * P, AHEAD = 2;
+        constexpr int STEPS = 4 * P, AHEAD = 2, MEANWHILE = 0;
         bf16x8 x[2][S::WIT], d[AHEAD + 1];
         const auto fetch_x = [&](int half, int b) { x[half][b] = transposed_operand(xtile + wi * S::WIT * 64, XPITCH, b, half * 16, lane); };
         const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = transposed_operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART + wo * 128, DPITCH, t % 2, t / (2 * P) * 16, lane); };
@@ -279,6 +280,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
                 even = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 4, 5), one, even, false);
                 dbsum[t % 2] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 6, 7), one, even, false);
             }
+            if (t == MEANWHILE) meanwhile();
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -302,8 +304,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         fill(round);
         sync();
         __builtin_amdgcn_s_setprio(3);  // products first: the other group's stores to LDS can wait, the operands cannot
-        load(round + 1);
-        multiply();
+        multiply([&]() { load(round + 1); });
         __builtin_amdgcn_s_setprio(0);
         sync();
     }

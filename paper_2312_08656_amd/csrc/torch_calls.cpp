@@ -20,17 +20,33 @@ decltype(&maxk_spgemm_fwd_narrow) forward_call;
 decltype(&maxk_spgemm_fwd_noalloc) forward_noalloc_call;
 decltype(&maxk_sspmm_bwd_narrow) backward_call;
 decltype(&maxk_cbsr_scatter) scatter_call;
+decltype(&maxk_mx_quantize) quantize_call;
+decltype(&maxk_mx_dequantize) dequantize_call;
+decltype(&maxk_mx_linear) linear_call;
+decltype(&maxk_mx_weight_grad_workspace) weight_grad_workspace_call;
+decltype(&maxk_mx_weight_grad) weight_grad_call;
+decltype(&maxk_mx_weight_grad_cbsr) weight_grad_cbsr_call;
+decltype(&maxk_mx_input_grad) input_grad_call;
+decltype(&maxk_mx_input_grad_cbsr) input_grad_cbsr_call;
 
 PyObject* check;  // (status, name of the call): raises; held for good
 
 void bind(const std::vector<uintptr_t>& at, const py::function& raise)
 {
-    TORCH_CHECK(at.size() == 5, "five addresses");
+    TORCH_CHECK(at.size() == 13, "thirteen addresses");
     topk_call = reinterpret_cast<decltype(topk_call)>(at[0]);
     forward_call = reinterpret_cast<decltype(forward_call)>(at[1]);
     forward_noalloc_call = reinterpret_cast<decltype(forward_noalloc_call)>(at[2]);
     backward_call = reinterpret_cast<decltype(backward_call)>(at[3]);
     scatter_call = reinterpret_cast<decltype(scatter_call)>(at[4]);
+    quantize_call = reinterpret_cast<decltype(quantize_call)>(at[5]);
+    dequantize_call = reinterpret_cast<decltype(dequantize_call)>(at[6]);
+    linear_call = reinterpret_cast<decltype(linear_call)>(at[7]);
+    weight_grad_workspace_call = reinterpret_cast<decltype(weight_grad_workspace_call)>(at[8]);
+    weight_grad_call = reinterpret_cast<decltype(weight_grad_call)>(at[9]);
+    weight_grad_cbsr_call = reinterpret_cast<decltype(weight_grad_cbsr_call)>(at[10]);
+    input_grad_call = reinterpret_cast<decltype(input_grad_call)>(at[11]);
+    input_grad_cbsr_call = reinterpret_cast<decltype(input_grad_cbsr_call)>(at[12]);
     Py_XDECREF(std::exchange(check, py::function(raise).release().ptr()));
 }
 
@@ -203,6 +219,139 @@ py::object aggregate_backward(uintptr_t g, int64_t N, const py::handle& dY_, con
     return py::cast(dH);
 }
 
+// ---- microscaled storage ----
+
+// A stored matrix [rows, din]: its codes and scales, or nulls.  din < 0: as many whole blocks as there are
+struct Stored {
+    const at::Tensor *codes, *scales;
+    int format;
+    int64_t din;
+    explicit operator bool() const { return codes != nullptr; }
+    uint8_t* code() const { return static_cast<uint8_t*>(codes->data_ptr()); }
+    uint8_t* scale() const { return static_cast<uint8_t*>(scales->data_ptr()); }
+};
+
+Stored stored(const py::handle& codes_, const py::handle& scales_, int64_t rows, int64_t din, bool only4)
+{
+    const at::Tensor *scales = matrix(scales_, rows, din < 0 ? -1 : (din + 31) / 32), *codes = matrix(codes_, rows, -1);
+    if (!scales || !codes || scales->scalar_type() != at::kByte) return {};
+    const bool four = codes->scalar_type() == at::kByte;
+    if (!four && (only4 || codes->scalar_type() != at::kChar)) return {};
+    if (codes->size(1) != scales->size(1) * (four ? 16 : 32)) return {};
+    return {codes, scales, four ? MAXK_MX_4 : MAXK_MX_8, din < 0 ? scales->size(1) * 32 : din};
+}
+
+const at::Tensor* vector(const py::handle& x, int64_t length)
+{
+    const at::Tensor* t = plain(x);
+    return t && t->dim() == 1 && t->is_contiguous() && t->size(0) == length && t->scalar_type() == at::kFloat ? t : nullptr;
+}
+
+bool mx_quantize(const py::handle& X_, const py::handle& codes_, const py::handle& scales_)
+{
+    const at::Tensor* X = matrix(X_, -1, -1);
+    if (!X || value_type(*X) < 0) return false;
+    const Stored to = stored(codes_, scales_, X->size(0), X->size(1), false);
+    if (!to) return false;
+    return made("maxk_mx_quantize", [&, s = stream()](const char*) {
+        return quantize_call(X->data_ptr(), value_type(*X), X->size(0), (int32_t)X->size(1), to.format, to.code(), to.scale(), s);
+    });
+}
+
+bool mx_dequantize(const py::handle& codes_, const py::handle& scales_, const py::handle& X_)
+{
+    const at::Tensor* X = matrix(X_, -1, -1);
+    if (!X || value_type(*X) < 0) return false;
+    const Stored from = stored(codes_, scales_, X->size(0), X->size(1), false);
+    if (!from) return false;
+    return made("maxk_mx_dequantize", [&, s = stream()](const char*) {
+        return dequantize_call(from.code(), from.scale(), from.format, X->size(0), (int32_t)X->size(1), X->data_ptr(), value_type(*X), s);
+    });
+}
+
+bool mx_linear(const py::handle& xc, const py::handle& xs, const py::handle& wc, const py::handle& ws, const py::handle& Y_, const py::handle& bias_)
+{
+    const at::Tensor* Y = matrix(Y_, -1, -1);
+    if (!Y || value_type(*Y) < 0) return false;
+    const Stored X = stored(xc, xs, Y->size(0), -1, true), W = stored(wc, ws, Y->size(1), -1, true);
+    const at::Tensor* bias = bias_.is_none() ? nullptr : vector(bias_, Y->size(1));
+    if (!X || !W || X.din != W.din || (!bias && !bias_.is_none())) return false;
+    return made("maxk_mx_linear", [&, s = stream()](const char*) {
+        return linear_call(X.code(), X.scale(), Y->size(0), W.code(), W.scale(), (int32_t)X.din, (int32_t)Y->size(1),
+                           bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, Y->data_ptr(), value_type(*Y), s);
+    });
+}
+
+// The gradient of a call: dense (index_ None) or CBSR
+struct Gradient {
+    const at::Tensor *values, *index;
+    explicit operator bool() const { return values != nullptr; }
+};
+
+Gradient gradient(const py::handle& values_, const py::handle& index_)
+{
+    const at::Tensor* values = matrix(values_, -1, -1);
+    if (!values || value_type(*values) < 0) return {};
+    if (index_.is_none()) return {values, nullptr};
+    const at::Tensor* index = matrix(index_, values->size(0), values->size(1));
+    if (!index || !index_bytes(*index) || values->scalar_type() != at::kFloat) return {};
+    return {values, index};
+}
+
+bool mx_weight_grad(const py::handle& codes_, const py::handle& scales_, const py::handle& values_, const py::handle& index_, const py::handle& dW_,
+                    const py::handle& db_, const py::handle& workspace_)
+{
+    const Gradient G = gradient(values_, index_);
+    const at::Tensor* dW = matrix(dW_, -1, -1);
+    if (!G || !dW || dW->scalar_type() != at::kFloat) return false;
+    const int64_t N = G.values->size(0), dout = dW->size(0), din = dW->size(1);
+    if (!G.index && G.values->size(1) != dout) return false;
+    const Stored X = stored(codes_, scales_, N, din, false);
+    const at::Tensor* db = db_.is_none() ? nullptr : vector(db_, dout);
+    if (!X || (!db && !db_.is_none()) || dout > MAXK_MX_MAX_DIM || din > MAXK_MX_MAX_DIM) return false;
+    at::Tensor own;
+    const at::Tensor* workspace = &own;
+    if (workspace_.is_none()) {
+        const int64_t need = weight_grad_workspace_call(N, (int32_t)din, (int32_t)dout);
+        if (need < 0) return false;
+        try {
+            own = at::empty({need}, dW->options().dtype(at::kByte));
+        } catch (const c10::Error&) {  // no memory: said by the call from Python
+            return false;
+        }
+    } else {
+        workspace = plain(workspace_);
+        if (!workspace || !workspace->is_contiguous() || workspace->scalar_type() != at::kByte) return false;
+    }
+    float *w = static_cast<float*>(dW->data_ptr()), *b = db ? static_cast<float*>(db->data_ptr()) : nullptr;
+    return made(G.index ? "maxk_mx_weight_grad_cbsr" : "maxk_mx_weight_grad", [&, s = stream()](const char*) {
+        if (G.index)
+            return weight_grad_cbsr_call(X.code(), X.scale(), X.format, N, (int32_t)din, (int32_t)dout, static_cast<const float*>(G.values->data_ptr()),
+                                         G.index->data_ptr(), index_bytes(*G.index), (int32_t)G.values->size(1), w, b, workspace->data_ptr(),
+                                         workspace->numel(), s);
+        return weight_grad_call(X.code(), X.scale(), X.format, N, (int32_t)din, (int32_t)dout, G.values->data_ptr(), value_type(*G.values), w, b,
+                                workspace->data_ptr(), workspace->numel(), s);
+    });
+}
+
+bool mx_input_grad(const py::handle& values_, const py::handle& index_, const py::handle& wc, const py::handle& ws, const py::handle& dX_)
+{
+    const Gradient G = gradient(values_, index_);
+    const at::Tensor* dX = matrix(dX_, -1, -1);
+    if (!G || !dX || value_type(*dX) < 0 || dX->size(0) != G.values->size(0)) return false;
+    const int64_t N = dX->size(0), din = dX->size(1);
+    const Stored W = stored(wc, ws, G.index ? -1 : G.values->size(1), din, true);
+    if (!W || W.codes->size(0) != W.scales->size(0)) return false;
+    const int64_t dout = W.codes->size(0);
+    return made(G.index ? "maxk_mx_input_grad_cbsr" : "maxk_mx_input_grad", [&, s = stream()](const char*) {
+        if (G.index)
+            return input_grad_cbsr_call(static_cast<const float*>(G.values->data_ptr()), G.index->data_ptr(), index_bytes(*G.index),
+                                        (int32_t)G.values->size(1), N, W.code(), W.scale(), (int32_t)din, (int32_t)dout, dX->data_ptr(), value_type(*dX), s);
+        return input_grad_call(G.values->data_ptr(), value_type(*G.values), N, W.code(), W.scale(), (int32_t)din, (int32_t)dout, dX->data_ptr(),
+                               value_type(*dX), s);
+    });
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_torch_calls, m)
@@ -215,4 +364,9 @@ PYBIND11_MODULE(_torch_calls, m)
     m.def("scatter", &scatter);
     m.def("aggregate_forward", &aggregate_forward);
     m.def("aggregate_backward", &aggregate_backward);
+    m.def("mx_quantize", &mx_quantize);
+    m.def("mx_dequantize", &mx_dequantize);
+    m.def("mx_linear", &mx_linear);
+    m.def("mx_weight_grad", &mx_weight_grad);
+    m.def("mx_input_grad", &mx_input_grad);
 }

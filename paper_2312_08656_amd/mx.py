@@ -56,6 +56,8 @@ def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int]:
 
 def maxk_mx_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
     """codes and scales are overwritten with X [N, din] (float32, bfloat16, float16) in the format of codes."""
+    if _b._FAST is not None and _b._FAST.mx_quantize(X, codes, scales):
+        return
     N, din = _matrix(X, "maxk_mx_quantize: X")
     fmt = _stored(codes, scales, N, din, "maxk_mx_quantize")
     _b._check(_b.load_library().maxk_mx_quantize(_b._dev(X, X.dtype, "X"), _value(X, "maxk_mx_quantize: X"), N, din, fmt,
@@ -65,6 +67,8 @@ def maxk_mx_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor)
 
 def maxk_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, X: torch.Tensor) -> None:
     """X [N, din] (float32, bfloat16, float16) is overwritten with what codes and scales stand for."""
+    if _b._FAST is not None and _b._FAST.mx_dequantize(codes, scales, X):
+        return
     N, din = _matrix(X, "maxk_mx_dequantize: X")
     fmt = _stored(codes, scales, N, din, "maxk_mx_dequantize")
     _b._check(_b.load_library().maxk_mx_dequantize(_b._dev(codes, codes.dtype, "codes"), _b._dev(scales, torch.uint8, "scales"), fmt, N, din,
@@ -82,6 +86,8 @@ def _same_width(a: torch.Tensor, b: torch.Tensor, what: str) -> int:
 def maxk_mx_linear(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, Y: torch.Tensor,
                    bias: Optional[torch.Tensor] = None) -> None:
     """Y [N, dout] (float32, bfloat16, float16) is overwritten with X W^T + bias, X [N, din] and W [dout, din] both in 4 bits."""
+    if _b._FAST is not None and _b._FAST.mx_linear(x_codes, x_scales, w_codes, w_scales, Y, bias):
+        return
     N, dout = _matrix(Y, "maxk_mx_linear: Y")
     din = _same_width(x_scales, w_scales, "maxk_mx_linear")
     _stored(x_codes, x_scales, N, din, "maxk_mx_linear: X", True)
@@ -122,6 +128,8 @@ def maxk_mx_weight_grad(codes: torch.Tensor, scales: torch.Tensor, dH: torch.Ten
     """dW [dout, din] and db [dout] (float32) are overwritten with dH^T X and the column sums of dH [N, dout] (float32, bfloat16,
     float16), X [N, din] stored in codes and scales.  workspace: uint8, from torch's allocator where none is given."""
     what = "maxk_mx_weight_grad"
+    if _b._FAST is not None and _b._FAST.mx_weight_grad(codes, scales, dH, None, dW, db, workspace):
+        return
     N, dout = _matrix(dH, f"{what}: dH")
     din, fmt = _weight_grad_shapes(codes, scales, N, dout, dW, db, what)
     args = (_b._dev(codes, codes.dtype, "codes"), _b._dev(scales, torch.uint8, "scales"), fmt, N, din, dout, _b._dev(dH, dH.dtype, "dH"),
@@ -134,6 +142,8 @@ def maxk_mx_weight_grad_cbsr(codes: torch.Tensor, scales: torch.Tensor, dXs: tor
                              db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """maxk_mx_weight_grad for the gradient that maxk_sspmm_bwd leaves: dXs [N, k] float32 at the columns sp_index [N, k]."""
     what = "maxk_mx_weight_grad_cbsr"
+    if _b._FAST is not None and _b._FAST.mx_weight_grad(codes, scales, dXs, sp_index, dW, db, workspace):
+        return
     N, k = _matrix(dXs, f"{what}: dXs")
     dout = _matrix(dW, f"{what}: dW")[0]
     din, fmt = _weight_grad_shapes(codes, scales, N, dout, dW, db, what)
@@ -154,6 +164,8 @@ def _index(sp_index: torch.Tensor, N: int, k: int, what: str) -> int:
 def maxk_mx_input_grad(dH: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, dX: torch.Tensor) -> None:
     """dX [N, din] (float32, bfloat16, float16) is overwritten with dH W, dH [N, dout] in any of these types, W [dout, din] in 4 bits."""
     what = "maxk_mx_input_grad"
+    if _b._FAST is not None and _b._FAST.mx_input_grad(dH, None, w_codes, w_scales, dX):
+        return
     N, dout = _matrix(dH, f"{what}: dH")
     rows, din = _matrix(dX, f"{what}: dX")
     _stored(w_codes, w_scales, dout, din, f"{what}: W", True)
@@ -167,6 +179,8 @@ def maxk_mx_input_grad(dH: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.
 def maxk_mx_input_grad_cbsr(dXs: torch.Tensor, sp_index: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, dX: torch.Tensor) -> None:
     """maxk_mx_input_grad for the gradient that maxk_sspmm_bwd leaves."""
     what = "maxk_mx_input_grad_cbsr"
+    if _b._FAST is not None and _b._FAST.mx_input_grad(dXs, sp_index, w_codes, w_scales, dX):
+        return
     N, k = _matrix(dXs, f"{what}: dXs")
     rows, din = _matrix(dX, f"{what}: dX")
     dout = _matrix(w_codes, f"{what}: W")[0]
