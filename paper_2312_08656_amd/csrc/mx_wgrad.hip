@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     float* const room = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int half = S::GR / 2; half >= 1; half /= 2) {
+        if (last - first <= half) continue;  // the upper groups had no step
         float* mine = room + ((group % half) * S::WAVES + w) * 64 * S::ACC + lane;
         if (group >= half && group < 2 * half) {
 #pragma unroll
@@ -425,9 +426,11 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
     p.otiles = (dout + S::TO - 1) / S::TO;
     p.itiles = (din + S::TI - 1) / S::TI;
     const int64_t tiles = (int64_t)p.otiles * p.itiles, steps = (N + kStep - 1) / kStep;
-    const int64_t resident = S::ACC > 64 ? 256 : 512;  // workgroups that run at a time
-    // each of them once, if every group has two steps
-    p.ranges = std::max<int64_t>(1, std::min(resident / tiles, steps / (2 * S::GR)));
+    const int64_t resident = S::ACC > 64 ? 256 : 512, rounds = (steps + S::GR - 1) / S::GR;  // workgroups that run at a time; rounds of a single range
+    // A round takes about 2 us, the second kernel 3 and more with more ranges: one range up to two rounds, a range each up to 32, then two rounds a range
+    // until no more workgroups run at a time.  (us, 256 x 256, CBSR k = 32: 256 rows 18.1 as one range / 14.5 as two; 4000 rows 19.8 as 31 / 21.3 as 63;
+    // 64 x 64, 1024 rows, k = 8: 15.7 as one / 12.4 as two.)
+    p.ranges = rounds <= 2 ? 1 : std::max<int64_t>(1, std::min(resident / tiles, std::max(std::min<int64_t>(rounds, 32), rounds / 2)));
     p.sums = p.ranges * tiles * S::TILE;
     p.dbsums = p.ranges * p.otiles * S::TO;
     return p;
