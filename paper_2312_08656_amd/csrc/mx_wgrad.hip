@@ -302,9 +302,12 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     }
     for (int round = 0; round < rounds; ++round) {
         fill(round);
+        if constexpr (CBSR) load(round + 1);  // (as many loads as a dense gradient's would hold up the barrier)
         sync();
         __builtin_amdgcn_s_setprio(3);  // products first: the other group's stores to LDS can wait, the operands cannot
-        multiply([&]() { load(round + 1); });
+        multiply([&]() {
+            if constexpr (!CBSR) load(round + 1);
+        });
         __builtin_amdgcn_s_setprio(0);
         sync();
     }
