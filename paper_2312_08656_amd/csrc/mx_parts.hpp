@@ -43,7 +43,7 @@ __device__ __forceinline__ void split(float x, float* part)
 // Tiles lie in LDS as the rows come, bf16, and are read transposed: a lane's operand is 8 rows of one column, and ds_read_b64_tr_b16 gives
 // 16 lanes 4 rows of 16 columns from 32 bytes of each of the rows.  The four rows of a read fall on different banks by the place of their bytes:
 // rows are multiples of 128 bytes, byte b of row r lies at b ^ 32 (r % 4).
-__device__ __forceinline__ int at_byte(int row, int byte, int pitch) { return row * pitch + (byte ^ (row & 3) << 5); }
+__device__ __forceinline__ int at_byte(int row, int byte, int pitch) { return row * pitch + (byte ^ (row & 3) << (pitch % 256 ? 5 : 6)); }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ s16x4 read_transposed(const uint8_t* p)
@@ -55,7 +55,7 @@ __device__ __forceinline__ s16x4 read_transposed(const uint8_t* p)
 __device__ __forceinline__ bf16x8 transposed_operand(const uint8_t* base, int pitch, int block, int row, int lane)
 {
     const int r = (lane >> 5) * 8 + (lane & 15) / 4, byte = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-    const uint8_t* p = base + at_byte(r, byte + (block & 1) * 64, pitch) + block / 2 * 128 + row * pitch;
+    const uint8_t* p = base + at_byte(r, byte + (block & 3) * 64, pitch) + block / 4 * 256 + row * pitch;
     const s16x4 low = read_transposed(p), high = read_transposed(p + 4 * pitch);
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
 }

@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     // the clearing is spread over the products and does not hold up the other group's first reads.
     constexpr bool CLEARS = CBSR && S::WI == 1;
     const auto clear_d = [&](int p, int half) {
-        uint8_t* to = dtile + p * DPART + (half * 16 + lane / 8) * DPITCH + wo * 128 + lane % 8 * 16;
+        uint8_t* to = dtile + p * DPART + at_byte(half * 16 + lane / 8, wo * 128 + lane % 8 * 16, DPITCH);
         *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
         *reinterpret_cast<uint4*>(to + 8 * DPITCH) = make_uint4(0, 0, 0, 0);
     };
@@ -256,8 +256,8 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
         // AHEAD products before they are needed, the second half's of X meanwhile
         constexpr int STEPS = 4 * P, AHEAD = 2, MEANWHILE = 0;
         bf16x8 x[2][S::WIT], d[AHEAD + 1];
-        const auto fetch_x = [&](int half, int b) { x[half][b] = transposed_operand(xtile + wi * S::WIT * 64, XPITCH, b, half * 16, lane); };
-        const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = transposed_operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART + wo * 128, DPITCH, t % 2, t / (2 * P) * 16, lane); };
+        const auto fetch_x = [&](int half, int b) { x[half][b] = transposed_operand(xtile, XPITCH, wi * S::WIT + b, half * 16, lane); };
+        const auto fetch_d = [&](int t) { d[t % (AHEAD + 1)] = transposed_operand(dtile + (P - 1 - t % (2 * P) / 2) * DPART, DPITCH, wo * 2 + t % 2, t / (2 * P) * 16, lane); };
 #pragma unroll
         for (int b = 0; b < S::WIT; ++b) fetch_x(0, b);
 #pragma unroll
