@@ -47,4 +47,4 @@ from .mx import (  # noqa: E402,F401
     mx_empty,
     mx_weight_grad_workspace,
 )
-from .autograd import MaxKAggregate, maxk_aggregate  # noqa: E402,F401
+from .autograd import MaxKAggregate, MaxKLayer, maxk_aggregate, maxk_layer  # noqa: E402,F401
