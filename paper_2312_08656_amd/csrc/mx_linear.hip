@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         Loaded<C> row;
-        load_blocks<C, true>(row, W, first, min(t * 16 + r, dout - 1 - first), g, nb);
+        load_blocks<C, true>(row, W, 0, min(first + t * 16 + r, dout - 1), g, nb);  // (the last wavefronts may lie past dout)
         w[t] = packed(row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
