@@ -3,6 +3,10 @@
 // The matrix instruction takes 4-bit codes with a scale byte for 32 products: 16 x 16 outputs over 128 columns, a lane holding one block of
 // either operand.  Rows are many and widths small, so a wavefront keeps 64 rows of W (all their columns) in its registers and walks
 // over the rows of X, 16 at a time; the next 16 are on their way meanwhile.  Wavefronts that share rows of X lie in one workgroup, so X is read through L1.
+//
+// Bound by the way to memory, mostly Y's way out: 2.4 M rows, 256 to 256, fp32 Y 541 us (2.78 GB, 5.1 TB/s, what a large copy reaches); 1 M rows
+// 181 us (6.4 TB/s, X in the Infinity Cache); 1.1 M rows, 384 to 256, bf16 Y 147 us (5.3 TB/s).  One row, 256 to 256: 3.9 us a call, two round trips to memory
+// and the launch.
 #include <algorithm>
 
 #include "mx_parts.hpp"
@@ -78,7 +82,7 @@ constexpr int kPad = 4;           // floats at the end of a row in LDS, so that 
 // WIDE: rows of Y are whole 16-byte pieces from a 16-byte boundary; else a column a lane.
 // ONCE: Y passes by L2.
 template <int C, int VT, bool WIDE, bool ONCE>
-__global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int64_t N, MxMatrix W, int nb, int dout, int gcols, int m,
+__global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int64_t N, MxMatrix W, int nb, int dout, int gcols, int m, bool pace,
                                                                  const float* __restrict__ bias, value_store_t<VT>* __restrict__ Y)
 {
     extern __shared__ __align__(16) float turned[];
@@ -130,6 +134,7 @@ __global__ void __launch_bounds__(64 * kMaxGroups) linear_kernel(MxMatrix X, int
         local_fence();  // the room of the step before was read before the one barrier, and is written after the next
     };
     const auto whole_step = [&]() {
+        if (pace) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
         make();
         value_store_t<VT>* out = Y + step * rows_step * dout + left;
 #pragma unroll
@@ -213,7 +218,8 @@ __global__ void __launch_bounds__(256) linear_long_kernel(MxMatrix X, int64_t N,
             }
 }
 
-// 3 for each of the 1024 SIMDs.  2.4 M rows, 256 to 256, fp32 Y: 833 / 665 / 655 / 648 us at 1 to 4; 29 k rows, 256 to 128, fp16: 7.4 at 2, 8.3, 9.6
+// 3 for each of the 1024 SIMDs.  us at 2600 / 3072 / 3400 wavefronts, 2.4 M rows, 256 to 256: 656 / 554 / 665 (whole workgroups a CU are faster than odd ones),
+// at 2048 689.
 constexpr int64_t kWaves = 3072;
 
 template <int C, int VT>
@@ -222,8 +228,12 @@ void launch_chunks(const MxMatrix& X, int64_t N, const MxMatrix& W, int nb, int 
     const int groups = (dout + kGroup - 1) / kGroup, sides = (groups + kMaxGroups - 1) / kMaxGroups, gcols = (groups + sides - 1) / sides, m = std::max(1, 4 / gcols);
     const int64_t steps = (N + kTileRows * m - 1) / (kTileRows * m), blocks = std::min(steps, std::max<int64_t>(1, kWaves / (gcols * m * sides)));
     const size_t lds = 2 * sizeof(float) * (size_t)(kTileRows * m) * (gcols * kGroup + kPad);
+    // Where X does not stay in the Infinity Cache its reads share the way to memory with Y's writes, and do better if a step waits for the writes of the
+    // one before.  us, with / without: 2.4 M rows, 256 to 256 541 / 617, bf16 Y 395 / 405; 1.2 M, 512 to 384 612 / 593; below that size 1.6 M, 256 to 256 304 / 300,
+    // 0.1 M 22.1 / 21.2.
+    const bool pace = (double)N * nb * 17 > kInfinityCache;
     const dim3 grid((unsigned)blocks, (unsigned)sides), block(64 * gcols * m);
-#define MAXK_LINEAR(WIDE, ONCE) hipLaunchKernelGGL((linear_kernel<C, VT, WIDE, ONCE>), grid, block, lds, s, X, N, W, nb, dout, gcols, m, bias, Y)
+#define MAXK_LINEAR(WIDE, ONCE) hipLaunchKernelGGL((linear_kernel<C, VT, WIDE, ONCE>), grid, block, lds, s, X, N, W, nb, dout, gcols, m, pace, bias, Y)
     if (dout * sizeof(*Y) % 16 != 0 || !aligned(Y, 16)) MAXK_LINEAR(false, false);
     else if (past_l2(N * dout * (int64_t)sizeof(*Y))) MAXK_LINEAR(true, true);
     else MAXK_LINEAR(true, false);
