@@ -71,7 +71,9 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
     const int rounds = (int)((last - first + S::GR - 1) / S::GR);
     uint8_t* const xtile = lds + group * GROUP;
     uint8_t* const dtile = xtile + XBYTES;
-    const bool sums_db = A.dbsums && i0 == 0;
+    // db is summed up once: for a dense gradient by the range's first tile, for a CBSR one, where it costs more, half each by the first two
+    const int itile = tile % A.itiles, second = CBSR && A.itiles > 1 ? 1 : 0;
+    const bool sums_db = A.dbsums && itile <= second, sums_even = A.dbsums && itile == 0, sums_odd = A.dbsums && itile == second;
     float* const dbcopies = reinterpret_cast<float*>(lds);
 
     // what this lane brings of X: 16 columns of a row
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
 #pragma unroll
             for (int b = 0; b < S::WIT; ++b)
                 sum[t % 2][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[t % (AHEAD + 1)], x[t / (2 * P)][b], sum[t % 2][b], 0, 0, 0);
-            if constexpr (CBSR) {  // db while the products run
+            if (CBSR && (t % 2 ? sums_odd : sums_even)) {  // db while the products run
                 const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
                 const bf16x8& y = d[t % (AHEAD + 1)];
                 float even = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(y, y, 0, 1), one, dbsum[t % 2], false);
@@ -358,6 +360,7 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
             float s = 0.f;
 #pragma unroll
             for (int g = 0; g < COPIES; ++g) s += dbcopies[g * S::TO + o];
+            if (!(o & 32 ? sums_odd : sums_even)) continue;
             if (A.ranges > 1) A.dbsums[range * A.otiles * S::TO + o0 + o] = s;
             else if (o0 + o < A.dout) A.db[o0 + o] = s;
         }
