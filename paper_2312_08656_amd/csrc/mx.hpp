@@ -8,7 +8,6 @@ namespace maxk {
 constexpr int kMxBlock = 32;  // columns that share a scale
 
 __host__ __device__ constexpr int mx_blocks(int dim) { return (dim + kMxBlock - 1) / kMxBlock; }
-__host__ __device__ constexpr int mx_block_bytes(int format) { return format == MAXK_MX_8 ? 32 : 16; }
 
 // 2^(s - 127), s = 255: NaN.  (the subnormal 2^-127 for s = 0)
 __device__ __forceinline__ float mx_scale(uint32_t s)
@@ -20,26 +19,6 @@ __device__ __forceinline__ float mx_scale(uint32_t s)
 __device__ __forceinline__ float mx8_unit(uint32_t s)
 {
     return __uint_as_float(s >= 7 ? (s == 255 ? 0x7FC00000u : (s - 6) << 23) : 0x00800000u >> (7 - s));
-}
-
-// magnitude of a 4-bit code: its two exponent bits and its last bit moved to their places in a float with a bias of 127, which is
-// 2^126 too small; exact for the subnormal 0.5 as well.  `code` may have higher bits set
-__device__ __forceinline__ float mx_e2m1(uint32_t code)
-{
-    const float a = __uint_as_float((code & 7u) << 22) * 0x1p126f;
-    return code & 8u ? -a : a;
-}
-
-// one stored value of a row
-template <int FMT>
-__device__ __forceinline__ float mx_value(const uint8_t* codes, const uint8_t* scales, int64_t row, int col, int nb)
-{
-    const float scale = mx_scale(scales[row * nb + col / kMxBlock]);
-    if constexpr (FMT == MAXK_MX_8) return (float)(int8_t)codes[row * nb * 32 + col] * 0x1p-6f * scale;
-    else {
-        const uint32_t two = codes[row * nb * 16 + col / 2];
-        return mx_e2m1(col & 1 ? two >> 4 : two) * scale;
-    }
 }
 
 // A gradient [N x dout]: dense (sp_index null), or k values a row at distinct columns

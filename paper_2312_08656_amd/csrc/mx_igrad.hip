@@ -1,9 +1,12 @@
 // Input gradient of the linear map with 4-bit weights (include/maxk.h): dX = dH W.
 //
 // On bf16 matrix instructions with fp32 accumulators.  W is exact in bf16, and a gradient is cut into bf16 parts that add up to it
-// exactly (fp32 three, fp16 two), so every product is exact and only the sums round.  A wavefront keeps the columns of dX that are its own,
-// 32 * IT of them, as rows of W in its registers and walks over tiles of 32 rows of dH, which the four wavefronts of a group bring to LDS
-// together: a CBSR gradient as its k values a row, spread over zeros.  A workgroup has two groups; one fills its tile while the other multiplies.
+// exactly (fp32 three, fp16 two), so every product is exact and only the sums round.  A wavefront has 32 * IT columns of dX: it keeps those columns of W in
+// its registers and walks over tiles of 32 rows of dH, which the four wavefronts of a group bring to LDS together: a CBSR gradient as its k values a
+// row, spread over zeros.  A workgroup has two groups; one fills its tile while the other multiplies.
+//
+// Bound by the way to memory where dH is dense (169 thousand rows, 256 x 256, fp32: 58 us, 6.0 TB/s), by the three parts' products beside the stores of dX where
+// it is CBSR (233 thousand, k = 32: 64 us; the products alone 37 at the clock it runs at, the stores 43).
 #include <algorithm>
 #include <type_traits>
 
@@ -355,10 +358,14 @@ maxk_status run(Args A, hipStream_t s)
 template <int KIND, int E = 1>
 maxk_status run_kind(const Args& A, hipStream_t s)
 {
-    const bool two = A.din > 128;  // columns of dX that four wavefronts hold, 32 each
+    // Four wavefronts hold 128 columns of dX, 32 each, or 256.  dH up to 256 columns leaves them the registers for two blocks of W each; up to 384 LDS holds two
+    // groups' tiles (200 thousand rows, CBSR k = 32, 384 -> 256 columns: 88 us, 162 as below); up to 512 one group of eight wavefronts fills and multiplies in turn
+    // (512 -> 384: 379 us); wider dH comes in chunks of 256 columns, and W anew with each.
+    const bool two = A.din > 128;
     if (A.dout <= 64) return two ? run<Shape<4, 2, 4, 2>, KIND, E>(A, s) : run<Shape<4, 1, 4, 2>, KIND, E>(A, s);
     if (A.dout <= 128) return two ? run<Shape<8, 2, 4, 2>, KIND, E>(A, s) : run<Shape<8, 1, 4, 2>, KIND, E>(A, s);
     if (A.dout <= 256) return two ? run<Shape<16, 2, 4, 2>, KIND, E>(A, s) : run<Shape<16, 1, 4, 2>, KIND, E>(A, s);
+    if (A.dout <= 384) return run<Shape<24, 1, 4, 2>, KIND, E>(A, s);
     if (A.dout <= 512) return run<Shape<32, 1, 8, 1>, KIND, E>(A, s);
     return run<Shape<16, 2, 4, 1>, KIND, E, true>(A, s);
 }

@@ -7,6 +7,11 @@
 // Rows are cut into ranges.  A workgroup owns a tile of dW for a range; it has GR groups of wavefronts that take its steps of 32 rows in
 // turn, each with its own tiles of X and dH in LDS, and adds the groups' sums up in LDS at the end.  With two groups one fills its tiles while the other
 // multiplies.  The ranges' sums go to the workspace and a second kernel adds them up, always in the same order.
+//
+// What it takes, 233 thousand rows, 256 x 256, CBSR k = 32: 82 us, of which 7 are the second kernel and 15 the start, the joining of groups and 32 MB of sums on
+// their way out; the rounds run at 60 % of what the three parts' products alone would (bound by the barriers between two groups that take turns, and by
+// LDS, half of its cycles busy).  Without db 80, without bringing dH and X 54 and those 22.  2.4 M rows, 64 x 64, dense fp32: 161 us (4.8 TB/s, memory); 717 thousand,
+// 384 x 384, bf16 from 4 bits: 281 us (2.5 TB/s; a phase of products is short against the way to memory, and the registers hold one round's values).
 #include <algorithm>
 #include <type_traits>
 
@@ -434,18 +439,22 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
     const int64_t tiles = (int64_t)p.otiles * p.itiles, steps = (N + kStep - 1) / kStep;
     const int64_t resident = S::ACC > 64 ? 256 : 512, rounds = (steps + S::GR - 1) / S::GR;  // workgroups that run at a time; rounds of a single range
     // A round takes about 2 us, the second kernel 3 and more with more ranges: one range up to two rounds, a range each up to 32, then two rounds a range
-    // until no more workgroups run at a time.  (us, 256 x 256, CBSR k = 32: 256 rows 18.1 as one range / 14.5 as two; 4000 rows 19.8 as 31 / 21.3 as 63;
-    // 64 x 64, 1024 rows, k = 8: 15.7 as one / 12.4 as two.)
-    p.ranges = rounds <= 2 ? 1 : std::max<int64_t>(1, std::min(resident / tiles, std::max(std::min<int64_t>(rounds, 32), rounds / 2)));
+    // until no more workgroups run at a time.  (us, 256 x 256, CBSR k = 32: 256 rows 18.1 as one range / 12.2 as four; 4000 rows 19.8 as 31 / 21.3 as 63;
+    // 64 x 64, 1024 rows, k = 8: 15.7 as one / 10.4 as four.)
+    // Every XCD has an eighth of the ranges, and of the workgroups that run: one range more than it has room for would take it twice as long (384 x 384: 6 tiles).
+    const int64_t most = tiles <= resident / 8 ? resident / 8 / tiles * 8 : std::max<int64_t>(1, resident / tiles);
+    p.ranges = rounds <= 2 ? 1 : std::min(most, std::max(std::min<int64_t>(rounds, 32), rounds / 2));
     p.sums = p.ranges * tiles * S::TILE;
     p.dbsums = p.ranges * p.otiles * S::TO;
     return p;
 }
 
-Plan plan(int64_t N, int din, int dout)
+// us, 200 thousand rows, as Middle / Wide: CBSR k = 8, 64 x 384 83 / 74, 256 x 384 155 / 129, 384 x 384 213 / 197, k = 64 107 / 80, 205 / 141, 283 / 215 (every tile
+// of dH looks at all entries of its rows); dense fp32 85 / 91, 147 / 165, 204 / 237, bf16 256 x 384 65 / 77.
+Plan plan(int64_t N, int din, int dout, bool cbsr)
 {
     if (din <= 64 && dout <= 64) return plan_of<Small>(0, N, din, dout);
-    if (dout > 128 && (dout + 255) / 256 * 2 == (dout + 127) / 128) return plan_of<Wide>(2, N, din, dout);
+    if (dout > 128 && (cbsr || (dout + 255) / 256 * 2 == (dout + 127) / 128)) return plan_of<Wide>(2, N, din, dout);
     return plan_of<Middle>(1, N, din, dout);
 }
 
@@ -496,8 +505,8 @@ maxk_status run_shape(const Args& A, int format, hipStream_t s)
 
 int64_t mx_weight_grad_workspace(int64_t N, int din, int dout)
 {
-    const Plan p = plan(N, din, dout);
-    return (p.sums + p.dbsums) * (int64_t)sizeof(float);
+    const Plan dense = plan(N, din, dout, false), cbsr = plan(N, din, dout, true);
+    return std::max(dense.sums + dense.dbsums, cbsr.sums + cbsr.dbsums) * (int64_t)sizeof(float);
 }
 
 maxk_status launch_mx_weight_grad(const MxMatrix& X, int64_t N, int din, int dout, const MxGrad& G, float* dW, float* db, float* workspace,
@@ -507,7 +516,7 @@ maxk_status launch_mx_weight_grad(const MxMatrix& X, int64_t N, int din, int dou
         if (const maxk_status st = launch_fill_zero(dW, (int64_t)dout * din, s)) return st;
         return db ? launch_fill_zero(db, dout, s) : MAXK_OK;
     }
-    const Plan p = plan(N, din, dout);
+    const Plan p = plan(N, din, dout, G.k > 0);
     const Args A = {X.codes, X.scales, N, din, dout, mx_blocks(din), G, p.ranges, p.otiles, p.itiles, workspace, db ? workspace + p.sums : nullptr, dW, db};
     return p.shape == 0 ? run_shape<Small>(A, X.format, s) : p.shape == 1 ? run_shape<Middle>(A, X.format, s) : run_shape<Wide>(A, X.format, s);
 }
