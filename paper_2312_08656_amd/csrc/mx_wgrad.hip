@@ -20,7 +20,8 @@
 namespace maxk {
 namespace {
 
-constexpr int kStep = 32;  // rows
+constexpr int kStep = 32;      // rows
+constexpr int kTogether = 16;  // ranges from which a range's tiles share an XCD
 
 // GR groups of WO x WI wavefronts; a wavefront has 64 rows of dW (columns of dH) and 32 * WIT of its columns
 template <int GR_, int WO_, int WI_, int WIT_>
@@ -66,10 +67,11 @@ __global__ void __launch_bounds__(S::THREADS) weight_grad_kernel(const Args A)
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / S::WAVES, w = wave % S::WAVES;
     const int wo = w % S::WO, wi = w / S::WO, me = w * 64 + lane;
-    // a range's tiles run on one XCD, whose L2 holds the rows that they share
+    // a range's tiles run on one XCD, whose L2 holds the rows that they share; few ranges spread over all of them
     const int tiles = A.otiles * A.itiles, at = blockIdx.x / 8, xcd = blockIdx.x % 8;
-    const int tile = at % tiles;
-    const int64_t range = (int64_t)(at / tiles) * 8 + xcd;
+    const bool together = A.ranges >= kTogether;
+    const int tile = (together ? at : (int)blockIdx.x) % tiles;
+    const int64_t range = together ? (int64_t)(at / tiles) * 8 + xcd : blockIdx.x / tiles;
     if (range >= A.ranges) return;
     const int o0 = tile / A.itiles * S::TO, i0 = tile % A.itiles * S::TI;
     const int64_t all_steps = (A.N + kStep - 1) / kStep, first = all_steps * range / A.ranges, last = all_steps * (range + 1) / A.ranges;
@@ -453,7 +455,12 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
 // of dH looks at all entries of its rows); dense fp32 85 / 91, 147 / 165, 204 / 237, bf16 256 x 384 65 / 77.
 Plan plan(int64_t N, int din, int dout, bool cbsr)
 {
-    if (din <= 64 && dout <= 64) return plan_of<Small>(0, N, din, dout);
+    // Few rows: small tiles, as long as all of them have a workgroup for every round, with eight groups a round.  us as above / so, CBSR k = 16: 256 x 256, 100 rows 13.4 /
+    // 8.9, 4000 18.2 / 13.6; 384 x 384, 1000 rows 19.8 / 12.7, 8000 30.7 / 34.4; 64 x 256, 8000 rows 19.5 / 11.7.  One tile of Middle is its equal up to 4000 rows
+    // (100 x 100: 500 rows 9.7 / 11.9, 8000 15.0 / 11.7).
+    const int64_t steps = (N + kStep - 1) / kStep, tiles = (int64_t)((din + 63) / 64) * ((dout + 63) / 64);
+    const bool few = (steps + Small::GR - 1) / Small::GR * tiles <= 512 && (din > 128 || dout > 128 || steps > 128);
+    if (few || (din <= 64 && dout <= 64)) return plan_of<Small>(0, N, din, dout);
     if (dout > 128 && (cbsr || (dout + 255) / 256 * 2 == (dout + 127) / 128)) return plan_of<Wide>(2, N, din, dout);
     return plan_of<Middle>(1, N, din, dout);
 }
@@ -461,7 +468,7 @@ Plan plan(int64_t N, int din, int dout, bool cbsr)
 template <class S, int FMT, int KIND, int E = 1>
 maxk_status run(const Args& A, hipStream_t s)
 {
-    const int64_t tiles = (int64_t)A.otiles * A.itiles, grid = (A.ranges + 7) / 8 * tiles * 8;
+    const int64_t tiles = (int64_t)A.otiles * A.itiles, grid = (A.ranges >= kTogether ? (A.ranges + 7) / 8 * 8 : A.ranges) * tiles;
     if (grid > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
     hipLaunchKernelGGL((weight_grad_kernel<S, FMT, KIND, E>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
     MAXK_LAUNCH_CHECK();
