@@ -105,3 +105,19 @@ def test_a_row_that_is_nan_and_gradients_of_infinity():
         assert not np.isfinite(host(db)[11]) and np.isfinite(np.delete(host(db), 11)).all()
         bad = ~np.isfinite(host(dX))
         assert bad[3].any() and not np.delete(bad, 3, axis=0).any()
+
+
+@pytest.mark.parametrize("k", [0, 12, 50, 200])
+@pytest.mark.parametrize("dout", [200, 257, 384, 516])
+def test_weight_gradients_of_many_rows(dout, k):
+    # row counts from which tiles of 128 and 256 columns of dH are taken, with widths that do not fill them
+    rng = np.random.default_rng(3 * dout + k)
+    for N, din, kinds in ((20001, 270, ("f32", "bf16", "f16")), (30070, 100, ("f32",))):
+        codes, scales, c, s = stored(mx.features(rng, N, din), 8)
+        X = mx.values(codes, scales, din)
+        for kind in kinds if k == 0 else ("f32",):
+            given, dH = gradient(rng, N, dout, k, kind, np.int16)
+            dW, db = torch.full((dout, din), float("nan"), device="cuda"), torch.full((dout,), float("nan"), device="cuda")
+            (maxk.maxk_mx_weight_grad_cbsr if k else maxk.maxk_mx_weight_grad)(c, s, *given, dW, db)
+            check(host(dW), dH.T @ X, np.abs(dH).T @ np.abs(X), N)
+            check(host(db), dH.sum(axis=0), np.abs(dH).sum(axis=0), N)
