@@ -457,7 +457,7 @@ Plan plan(int64_t N, int din, int dout, bool cbsr)
 {
     // Few rows: small tiles, as long as all of them have a workgroup for every round, with eight groups a round.  us as above / so, CBSR k = 16: 256 x 256, 100 rows 13.4 /
     // 8.9, 4000 18.2 / 13.6; 384 x 384, 1000 rows 19.8 / 12.7, 8000 30.7 / 34.4; 64 x 256, 8000 rows 19.5 / 11.7.  One tile of Middle is its equal up to 4000 rows
-    // (100 x 100: 500 rows 9.7 / 11.9, 8000 15.0 / 11.7).
+    // (100 x 100: 500 rows 9.7 / 11.9, 8000 15.0 / 11.7).  Dense fp32: 256 x 256, 100 rows 12.7 / 8.0, 4000 17.9 / 12.7; 384 x 384, 1000 rows 14.9 / 11.3.
     const int64_t steps = (N + kStep - 1) / kStep, tiles = (int64_t)((din + 63) / 64) * ((dout + 63) / 64);
     const bool few = (steps + Small::GR - 1) / Small::GR * tiles <= 512 && (din > 128 || dout > 128 || steps > 128);
     if (few || (din <= 64 && dout <= 64)) return plan_of<Small>(0, N, din, dout);
@@ -479,7 +479,7 @@ template <class S>
 maxk_status run_shape(const Args& A, int format, hipStream_t s)
 {
     maxk_status st;
-    constexpr int WIDEST = S::TO == 128 ? 16 : 8;  // 64 columns of dH have k up to 64; 256 and 16 entries would not fit the registers
+    constexpr int WIDEST = S::TO == 128 ? 16 : 8;  // (16 would not fit Wide's registers, and Small's rows are few or have k up to 64)
     const bool pieces = aligned(A.G.values, 16) && A.dout * (A.G.value_type == MAXK_VALUE_F32 ? 4 : 2) % 16 == 0;  // rows of whole 16-byte pieces
 #define MAXK_ENTRIES(KIND)                                                                                                                            \
     st = A.G.k <= 32   ? (format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND, 4>(A, s) : run<S, MAXK_MX_4, KIND, 4>(A, s))                                  \
