@@ -218,9 +218,9 @@ __global__ void __launch_bounds__(256) linear_long_kernel(MxMatrix X, int64_t N,
             }
 }
 
-// 3 for each of the 1024 SIMDs.  us at 2600 / 3072 / 3400 wavefronts, 2.4 M rows, 256 to 256: 656 / 554 / 665 (whole workgroups a CU are faster than odd ones),
+// 3 for each of the 1024 SIMDs.  us at 2600 / 3 x 1024 / 3400 wavefronts, 2.4 M rows, 256 to 256: 656 / 554 / 665 (whole workgroups a CU are faster than odd ones),
 // at 2048 689.
-constexpr int64_t kWaves = 3072;
+constexpr int64_t kWaves = 3 * 1024;
 
 template <int C, int VT>
 void launch_chunks(const MxMatrix& X, int64_t N, const MxMatrix& W, int nb, int dout, const float* bias, value_store_t<VT>* Y, hipStream_t s)
