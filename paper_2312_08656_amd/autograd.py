@@ -2,7 +2,8 @@
 
 Forward : maxk_topk_cbsr -> maxk_spgemm_fwd.
 Backward: maxk_sspmm_bwd (gradient only at the CBSR support) -> maxk_cbsr_scatter back to dense.
-Every step runs in the HIP kernels; torch provides tensors, the stream and the autograd tape.
+Every step runs in the HIP kernels; torch provides tensors, the stream and the autograd tape.  What the kernels write is not on the tape, so a second
+derivative through either function is refused.
 
 A layer, Y = A * MaxK_k(X W^T + b), keeps its input in 8 or 4 bits for the weight gradient, which is taken from the CBSR gradient and the
 stored codes: neither X in 32 bits nor a dense dH is kept or made for it.
@@ -12,6 +13,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as _b
 from . import mx as _mx
@@ -28,6 +30,7 @@ class MaxKAggregate(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY: torch.Tensor):
         (sp_index,) = ctx.saved_tensors
         dH = _b.aggregate_backward(ctx.graph, dY.contiguous(), sp_index, ctx.dim, ctx.k)
@@ -35,7 +38,7 @@ class MaxKAggregate(torch.autograd.Function):
 
 
 def maxk_aggregate(H: torch.Tensor, graph: _b.MaxKGraph, k: int) -> torch.Tensor:
-    """Y = A * MaxK_k(H), differentiable with respect to H."""
+    """Y = A * MaxK_k(H), differentiable (once) with respect to H."""
     return MaxKAggregate.apply(H, graph, k)
 
 
@@ -65,6 +68,7 @@ class MaxKLayer(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY: torch.Tensor):
         sp_index, codes, scales, *weights = ctx.saved_tensors
         N, din, dout = ctx.sizes
@@ -88,7 +92,7 @@ class MaxKLayer(torch.autograd.Function):
 
 
 def maxk_layer(X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int = 8) -> torch.Tensor:
-    """Y = A * MaxK_k(X W^T + b) for X [N, din], W [dout, din], b [dout] or None (float32), differentiable with respect to all three.
+    """Y = A * MaxK_k(X W^T + b) for X [N, din], W [dout, din], b [dout] or None (float32), differentiable (once) with respect to all three.
 
     bits=8: the product is torch's, in float32; X is kept in 8 bits, and dW is that of the kept values.
     bits=4: X and W are rounded to 4 bits, the product and both its gradients are of the rounded values (straight through the rounding).
