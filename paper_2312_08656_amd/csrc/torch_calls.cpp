@@ -221,6 +221,13 @@ py::object aggregate_backward(uintptr_t g, int64_t N, const py::handle& dY_, con
 
 // ---- microscaled storage ----
 
+// matrix() of a width that the calls take, and 32 bits hold
+const at::Tensor* sized(const py::handle& x, int64_t rows, int64_t cols)
+{
+    const at::Tensor* t = matrix(x, rows, cols);
+    return t && t->size(1) <= MAXK_MX_MAX_DIM ? t : nullptr;
+}
+
 // A stored matrix [rows, din]: its codes and scales, or nulls.  din < 0: as many whole blocks as there are
 struct Stored {
     const at::Tensor *codes, *scales;
@@ -237,7 +244,7 @@ Stored stored(const py::handle& codes_, const py::handle& scales_, int64_t rows,
     if (!scales || !codes || scales->scalar_type() != at::kByte) return {};
     const bool four = codes->scalar_type() == at::kByte;
     if (!four && (only4 || codes->scalar_type() != at::kChar)) return {};
-    if (codes->size(1) != scales->size(1) * (four ? 16 : 32)) return {};
+    if (codes->size(1) != scales->size(1) * (four ? 16 : 32) || (din < 0 && scales->size(1) > MAXK_MX_MAX_DIM / 32)) return {};
     return {codes, scales, four ? MAXK_MX_4 : MAXK_MX_8, din < 0 ? scales->size(1) * 32 : din};
 }
 
@@ -249,7 +256,7 @@ const at::Tensor* vector(const py::handle& x, int64_t length)
 
 bool mx_quantize(const py::handle& X_, const py::handle& codes_, const py::handle& scales_)
 {
-    const at::Tensor* X = matrix(X_, -1, -1);
+    const at::Tensor* X = sized(X_, -1, -1);
     if (!X || value_type(*X) < 0) return false;
     const Stored to = stored(codes_, scales_, X->size(0), X->size(1), false);
     if (!to) return false;
@@ -260,7 +267,7 @@ bool mx_quantize(const py::handle& X_, const py::handle& codes_, const py::handl
 
 bool mx_dequantize(const py::handle& codes_, const py::handle& scales_, const py::handle& X_)
 {
-    const at::Tensor* X = matrix(X_, -1, -1);
+    const at::Tensor* X = sized(X_, -1, -1);
     if (!X || value_type(*X) < 0) return false;
     const Stored from = stored(codes_, scales_, X->size(0), X->size(1), false);
     if (!from) return false;
@@ -271,7 +278,7 @@ bool mx_dequantize(const py::handle& codes_, const py::handle& scales_, const py
 
 bool mx_linear(const py::handle& xc, const py::handle& xs, const py::handle& wc, const py::handle& ws, const py::handle& Y_, const py::handle& bias_)
 {
-    const at::Tensor* Y = matrix(Y_, -1, -1);
+    const at::Tensor* Y = sized(Y_, -1, -1);
     if (!Y || value_type(*Y) < 0) return false;
     const Stored X = stored(xc, xs, Y->size(0), -1, true), W = stored(wc, ws, Y->size(1), -1, true);
     const at::Tensor* bias = bias_.is_none() ? nullptr : vector(bias_, Y->size(1));
@@ -290,7 +297,7 @@ struct Gradient {
 
 Gradient gradient(const py::handle& values_, const py::handle& index_)
 {
-    const at::Tensor* values = matrix(values_, -1, -1);
+    const at::Tensor* values = sized(values_, -1, -1);
     if (!values || value_type(*values) < 0) return {};
     if (index_.is_none()) return {values, nullptr};
     const at::Tensor* index = matrix(index_, values->size(0), values->size(1));
@@ -302,13 +309,13 @@ bool mx_weight_grad(const py::handle& codes_, const py::handle& scales_, const p
                     const py::handle& db_, const py::handle& workspace_)
 {
     const Gradient G = gradient(values_, index_);
-    const at::Tensor* dW = matrix(dW_, -1, -1);
+    const at::Tensor* dW = sized(dW_, -1, -1);
     if (!G || !dW || dW->scalar_type() != at::kFloat) return false;
     const int64_t N = G.values->size(0), dout = dW->size(0), din = dW->size(1);
     if (!G.index && G.values->size(1) != dout) return false;
     const Stored X = stored(codes_, scales_, N, din, false);
     const at::Tensor* db = db_.is_none() ? nullptr : vector(db_, dout);
-    if (!X || (!db && !db_.is_none()) || dout > MAXK_MX_MAX_DIM || din > MAXK_MX_MAX_DIM) return false;
+    if (!X || (!db && !db_.is_none()) || dout > MAXK_MX_MAX_DIM) return false;
     at::Tensor own;
     const at::Tensor* workspace = &own;
     if (workspace_.is_none()) {
@@ -337,12 +344,13 @@ bool mx_weight_grad(const py::handle& codes_, const py::handle& scales_, const p
 bool mx_input_grad(const py::handle& values_, const py::handle& index_, const py::handle& wc, const py::handle& ws, const py::handle& dX_)
 {
     const Gradient G = gradient(values_, index_);
-    const at::Tensor* dX = matrix(dX_, -1, -1);
+    const at::Tensor* dX = sized(dX_, -1, -1);
     if (!G || !dX || value_type(*dX) < 0 || dX->size(0) != G.values->size(0)) return false;
     const int64_t N = dX->size(0), din = dX->size(1);
     const Stored W = stored(wc, ws, G.index ? -1 : G.values->size(1), din, true);
     if (!W || W.codes->size(0) != W.scales->size(0)) return false;
     const int64_t dout = W.codes->size(0);
+    if (dout > MAXK_MX_MAX_DIM) return false;
     return made(G.index ? "maxk_mx_input_grad_cbsr" : "maxk_mx_input_grad", [&, s = stream()](const char*) {
         if (G.index)
             return input_grad_cbsr_call(static_cast<const float*>(G.values->data_ptr()), G.index->data_ptr(), index_bytes(*G.index),

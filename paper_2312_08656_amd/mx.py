@@ -14,6 +14,8 @@ from . import binding as _b
 from .binding import MaxKError
 
 MX_8, MX_4 = 0, 1
+_MAX_DIM = 65536  # MAXK_MX_MAX_DIM
+_UNSUPPORTED = -2
 _FORMAT = {torch.int8: MX_8, torch.uint8: MX_4}
 
 
@@ -48,10 +50,17 @@ def _value(t: torch.Tensor, what: str) -> int:
     return _b._VALUE_TYPE[t.dtype]
 
 
+def _width(n: int, what: str) -> int:
+    """n, refused here where the library's 32 bits might not hold it."""
+    if n > _MAX_DIM:
+        _b._check(_UNSUPPORTED, what)
+    return n
+
+
 def _matrix(t: torch.Tensor, what: str) -> Tuple[int, int]:
     if t.dim() != 2:
         raise MaxKError(f"{what}: expected a matrix")
-    return t.shape[0], t.shape[1]
+    return t.shape[0], _width(t.shape[1], what)
 
 
 def maxk_mx_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
@@ -80,7 +89,7 @@ def _same_width(a: torch.Tensor, b: torch.Tensor, what: str) -> int:
     """Columns of two 4-bit matrices, rounded up to whole blocks (what lies past din is zero in either)."""
     if _matrix(a, what)[1] != _matrix(b, what)[1]:
         raise MaxKError(f"{what}: the operands' blocks do not match")
-    return 32 * a.shape[1]
+    return _width(32 * a.shape[1], what)
 
 
 def maxk_mx_linear(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, Y: torch.Tensor,
@@ -117,9 +126,10 @@ def _workspace(workspace: Optional[torch.Tensor], N: int, din: int, dout: int, d
 
 def mx_weight_grad_workspace(N: int, din: int, dout: int) -> int:
     """Bytes that maxk_mx_weight_grad and maxk_mx_weight_grad_cbsr need as `workspace` (a uint8 tensor)."""
-    need = int(_b.load_library().maxk_mx_weight_grad_workspace(N, din, dout))
+    what = "maxk_mx_weight_grad_workspace"
+    need = int(_b.load_library().maxk_mx_weight_grad_workspace(N, _width(din, what), _width(dout, what)))
     if need < 0:
-        _b._check(need, "maxk_mx_weight_grad_workspace")
+        _b._check(need, what)
     return need
 
 
@@ -145,7 +155,7 @@ def maxk_mx_weight_grad_cbsr(codes: torch.Tensor, scales: torch.Tensor, dXs: tor
     if _b._FAST is not None and _b._FAST.mx_weight_grad(codes, scales, dXs, sp_index, dW, db, workspace):
         return
     N, k = _matrix(dXs, f"{what}: dXs")
-    dout = _matrix(dW, f"{what}: dW")[0]
+    dout = _width(_matrix(dW, f"{what}: dW")[0], f"{what}: dW")
     din, fmt = _weight_grad_shapes(codes, scales, N, dout, dW, db, what)
     ib = _index(sp_index, N, k, what)
     args = (_b._dev(codes, codes.dtype, "codes"), _b._dev(scales, torch.uint8, "scales"), fmt, N, din, dout, _b._dev(dXs, torch.float32, "dXs"),
@@ -183,7 +193,7 @@ def maxk_mx_input_grad_cbsr(dXs: torch.Tensor, sp_index: torch.Tensor, w_codes: 
         return
     N, k = _matrix(dXs, f"{what}: dXs")
     rows, din = _matrix(dX, f"{what}: dX")
-    dout = _matrix(w_codes, f"{what}: W")[0]
+    dout = _width(_matrix(w_codes, f"{what}: W")[0], f"{what}: W")
     _stored(w_codes, w_scales, dout, din, f"{what}: W", True)
     ib = _index(sp_index, N, k, what)
     if rows != N:
