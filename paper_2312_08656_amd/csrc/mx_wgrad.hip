@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(256) add_ranges_kernel(const Args A)
 struct Plan {
     int shape;  // 0 Small, 1 Middle, 2 Wide
     int otiles, itiles;
-    int64_t ranges, sums, dbsums;  // floats of the workspace
+    int64_t ranges, sums, dbsums;  // floats of the workspace: none where one range writes dW and db itself
 };
 
 template <class S>
@@ -446,8 +446,8 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
     // Every XCD has an eighth of the ranges, and of the workgroups that run: one range more than it has room for would take it twice as long (384 x 384: 6 tiles).
     const int64_t most = tiles <= resident / 8 ? resident / 8 / tiles * 8 : std::max<int64_t>(1, resident / tiles);
     p.ranges = rounds <= 2 ? 1 : std::min(most, std::max(std::min<int64_t>(rounds, 32), rounds / 2));
-    p.sums = p.ranges * tiles * S::TILE;
-    p.dbsums = p.ranges * p.otiles * S::TO;
+    p.sums = p.ranges > 1 ? p.ranges * tiles * S::TILE : 0;
+    p.dbsums = p.ranges > 1 ? p.ranges * p.otiles * S::TO : 0;
     return p;
 }
 
@@ -513,7 +513,7 @@ maxk_status run_shape(const Args& A, int format, hipStream_t s)
 int64_t mx_weight_grad_workspace(int64_t N, int din, int dout)
 {
     const Plan dense = plan(N, din, dout, false), cbsr = plan(N, din, dout, true);
-    return std::max(dense.sums + dense.dbsums, cbsr.sums + cbsr.dbsums) * (int64_t)sizeof(float);
+    return std::max<int64_t>({16, (dense.sums + dense.dbsums) * (int64_t)sizeof(float), (cbsr.sums + cbsr.dbsums) * (int64_t)sizeof(float)});
 }
 
 maxk_status launch_mx_weight_grad(const MxMatrix& X, int64_t N, int din, int dout, const MxGrad& G, float* dW, float* db, float* workspace,
