@@ -42,9 +42,15 @@ def maxk_aggregate(H: torch.Tensor, graph: _b.MaxKGraph, k: int) -> torch.Tensor
     return MaxKAggregate.apply(H, graph, k)
 
 
+_HALVES = (torch.bfloat16, torch.float16)
+
+
 class MaxKLayer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int):
+        if torch.is_autocast_enabled(X.device.type):
+            with torch.autocast(X.device.type, enabled=False):
+                return MaxKLayer.forward(ctx, *(t.float() if t is not None and t.dtype in _HALVES else t for t in (X, W, b)), graph, k, bits)
         if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1] or X.dtype != torch.float32 or W.dtype != torch.float32:
             raise _b.MaxKError("maxk_layer: X [N, din] and W [dout, din] must be float32 matrices of one width")
         if bits not in (8, 4):
@@ -93,6 +99,8 @@ class MaxKLayer(torch.autograd.Function):
 
 def maxk_layer(X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int = 8) -> torch.Tensor:
     """Y = A * MaxK_k(X W^T + b) for X [N, din], W [dout, din], b [dout] or None (float32), differentiable (once) with respect to all three.
+
+    Under autocast 16-bit arguments are widened, and the layer stays one of float32.
 
     bits=8: the product is torch's, in float32; X is kept in 8 bits, and dW is that of the kept values.
     bits=4: X and W are rounded to 4 bits, the product and both its gradients are of the rounded values (straight through the rounding).

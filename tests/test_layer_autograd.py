@@ -66,7 +66,8 @@ def calls(monkeypatch):
     for module, names in ((autograd._b, ("aggregate_forward", "aggregate_backward", "maxk_sspmm_bwd", "maxk_cbsr_scatter")),
                           (autograd._mx, ("maxk_mx_quantize", "maxk_mx_linear", "maxk_mx_weight_grad_cbsr", "maxk_mx_input_grad_cbsr"))):
         for name in names:
-            monkeypatch.setattr(module, name, torch.no_grad()(getattr(stand_ins, name)))  # (a kernel's writes are not on the tape)
+            # a kernel's writes are not on the tape, and autocast does not change what it computes
+            monkeypatch.setattr(module, name, torch.no_grad()(torch.autocast("cpu", enabled=False)(getattr(stand_ins, name))))
     return stand_ins
 
 
@@ -100,3 +101,44 @@ def test_second_derivatives_of_the_layer_are_refused(calls, bits, needs):
         _penalised(maxk.maxk_layer(*args, None, 8, bits), wanted).backward()
     again = torch.autograd.grad(maxk.maxk_layer(*args, None, 8, bits).sum(), wanted, create_graph=True)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("given", [torch.float32, torch.bfloat16])
+def test_the_layer_is_one_of_float32_under_autocast(calls, bits, given):
+    X, W, b = _operands()
+    x = X.detach().to(given)  # as a layer before it leaves it there
+    dY = torch.randn(12, 24, generator=torch.Generator().manual_seed(3))
+    plain = [x.float().requires_grad_(True), W, b]
+    Y = maxk.maxk_layer(*plain, None, 8, bits)
+    want = torch.autograd.grad(Y, plain, dY)
+    args = [x.requires_grad_(True), W, b]
+    with torch.autocast("cpu", dtype=torch.bfloat16):
+        Y2 = maxk.maxk_layer(*args, None, 8, bits)
+        inside = torch.autograd.grad(Y2, args, dY, retain_graph=True)
+    outside = torch.autograd.grad(Y2, args, dY)
+    assert torch.equal(Y2, Y)
+    for got in (inside, outside):
+        assert [g.dtype for g in got] == [given, torch.float32, torch.float32]
+        assert all(torch.equal(g, w.to(g.dtype)) for g, w in zip(got, want))
+    with pytest.raises(maxk.MaxKError):
+        maxk.maxk_layer(X.detach().bfloat16(), W, b, None, 8, bits)  # as before, where autocast is off
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 4])
+def test_the_layer_trains_under_autocast_on_the_device(bits):
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    N, din, dout, k = 200, 40, 48, 8
+    col = torch.randint(N, (N * 5,), generator=gen, device="cuda").to(torch.int32)
+    graph = maxk.maxk_graph_create(torch.arange(0, 5 * N + 1, 5, device="cuda", dtype=torch.int32), col, torch.rand(N * 5, generator=gen, device="cuda"))
+    X, W0, W, b = (torch.randn(s, generator=gen, device="cuda") for s in ((N, 30), (din, 30), (dout, din), (dout,)))
+    W.requires_grad_(True), b.requires_grad_(True), W0.requires_grad_(True)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        h = torch.nn.functional.linear(X, W0)
+        assert h.dtype == torch.bfloat16
+        Y = maxk.maxk_layer(h, W, b, graph, k, bits)
+    assert torch.equal(Y, maxk.maxk_layer(h.float(), W, b, graph, k, bits))
+    want = torch.autograd.grad(maxk.maxk_layer(h.float(), W, b, graph, k, bits).square().sum(), [W, b])
+    Y.square().sum().backward()
+    assert torch.equal(W.grad, want[0]) and torch.equal(b.grad, want[1]) and bool(W0.grad.any())
