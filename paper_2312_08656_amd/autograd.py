@@ -53,6 +53,8 @@ class MaxKLayer(torch.autograd.Function):
                 return MaxKLayer.forward(ctx, *(t.float() if t is not None and t.dtype in _HALVES else t for t in (X, W, b)), graph, k, bits)
         if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1] or X.dtype != torch.float32 or W.dtype != torch.float32:
             raise _b.MaxKError("maxk_layer: X [N, din] and W [dout, din] must be float32 matrices of one width")
+        if b is not None and (b.shape != W.shape[:1] or b.dtype != torch.float32):
+            raise _b.MaxKError("maxk_layer: b must be float32 [dout]")
         if bits not in (8, 4):
             raise _b.MaxKError("maxk_layer: bits must be 8 or 4")
         X, W = X.contiguous(), W.contiguous()

@@ -142,3 +142,14 @@ def test_the_layer_trains_under_autocast_on_the_device(bits):
     want = torch.autograd.grad(maxk.maxk_layer(h.float(), W, b, graph, k, bits).square().sum(), [W, b])
     Y.square().sum().backward()
     assert torch.equal(W.grad, want[0]) and torch.equal(b.grad, want[1]) and bool(W0.grad.any())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_a_bias_is_one_of_the_columns(calls, bits):
+    X, W, b = (t.detach() for t in _operands())
+    for bad in (b[:1], b[:-1], b[0], b.reshape(1, -1), b.expand(12, 24), b.double(), b.bfloat16()):
+        with pytest.raises(maxk.MaxKError, match="maxk_layer: b must be"):
+            maxk.maxk_layer(X, W, bad, None, 8, bits)
+    strided = torch.stack([b, b], dim=1)[:, 0]
+    assert torch.equal(maxk.maxk_layer(X, W, strided, None, 8, bits), maxk.maxk_layer(X, W, b, None, 8, bits))
+    assert torch.isfinite(maxk.maxk_layer(X, W, None, None, 8, bits)).all()
