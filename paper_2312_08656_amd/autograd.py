@@ -47,10 +47,10 @@ _HALVES = (torch.bfloat16, torch.float16)
 
 class MaxKLayer(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int):
+    def forward(ctx, X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int, tape: bool = True):
         if torch.is_autocast_enabled(X.device.type):
             with torch.autocast(X.device.type, enabled=False):
-                return MaxKLayer.forward(ctx, *(t.float() if t is not None and t.dtype in _HALVES else t for t in (X, W, b)), graph, k, bits)
+                return MaxKLayer.forward(ctx, *(t.float() if t is not None and t.dtype in _HALVES else t for t in (X, W, b)), graph, k, bits, tape)
         if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[1] or X.dtype != torch.float32 or W.dtype != torch.float32:
             raise _b.MaxKError("maxk_layer: X [N, din] and W [dout, din] must be float32 matrices of one width")
         if b is not None and (b.shape != W.shape[:1] or b.dtype != torch.float32):
@@ -59,8 +59,10 @@ class MaxKLayer(torch.autograd.Function):
             raise _b.MaxKError("maxk_layer: bits must be 8 or 4")
         X, W = X.contiguous(), W.contiguous()
         (N, din), dout = X.shape, W.shape[0]
-        stored = _mx.mx_empty(N, din, bits, X.device)
-        _mx.maxk_mx_quantize(X, *stored)
+        stored = (None, None)
+        if bits == 4 or (tape and any(ctx.needs_input_grad[1:3])):  # in 8 bits only dW and db read the codes
+            stored = _mx.mx_empty(N, din, bits, X.device)
+            _mx.maxk_mx_quantize(X, *stored)
         if bits == 8:
             weights = (W,)
             H = torch.mm(X, W.t()) if b is None else torch.addmm(b, X, W.t())
@@ -96,7 +98,7 @@ class MaxKLayer(torch.autograd.Function):
                 dH = torch.empty((N, dout), dtype=torch.float32, device=dY.device)
                 _b.maxk_cbsr_scatter(dXs, sp_index, dH)
                 torch.mm(dH, weights[0], out=dX)
-        return dX, dW if need_W else None, db, None, None, None
+        return dX, dW if need_W else None, db, None, None, None, None
 
 
 def maxk_layer(X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], graph: _b.MaxKGraph, k: int, bits: int = 8) -> torch.Tensor:
@@ -107,4 +109,4 @@ def maxk_layer(X: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor], grap
     bits=8: the product is torch's, in float32; X is kept in 8 bits, and dW is that of the kept values.
     bits=4: X and W are rounded to 4 bits, the product and both its gradients are of the rounded values (straight through the rounding).
     """
-    return MaxKLayer.apply(X, W, b, graph, k, bits)
+    return MaxKLayer.apply(X, W, b, graph, k, bits, torch.is_grad_enabled())  # (False within forward in any case)

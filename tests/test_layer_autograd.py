@@ -153,3 +153,24 @@ def test_a_bias_is_one_of_the_columns(calls, bits):
     strided = torch.stack([b, b], dim=1)[:, 0]
     assert torch.equal(maxk.maxk_layer(X, W, strided, None, 8, bits), maxk.maxk_layer(X, W, b, None, 8, bits))
     assert torch.isfinite(maxk.maxk_layer(X, W, None, None, 8, bits)).all()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_no_checkpoint_where_nothing_will_read_it(calls, bits):
+    def made(needs, grad=True):
+        calls.made.clear()
+        with torch.set_grad_enabled(grad):
+            Y = maxk.maxk_layer(*_operands(needs), None, 8, bits)
+        quantized = calls.made.count("quantize")
+        if Y.requires_grad:
+            Y.sum().backward()
+        return quantized, Y.detach()
+
+    without = 0 if bits == 8 else 2  # in 4 bits the product itself reads the codes of X and W
+    kept, Y = made((True, True, True))
+    assert kept == without + (bits == 8)
+    for needs, grad, count in (((False, False, False), True, without), ((True, False, False), True, without), ((True, True, True), False, without),
+                               ((False, True, False), True, kept), ((False, False, True), True, kept)):
+        got = made(needs, grad)
+        assert got[0] == count, (needs, grad)
+        assert torch.equal(got[1], Y)
