@@ -364,10 +364,12 @@ maxk_status run_kind(const Args& A, hipStream_t s)
     const bool two = A.din > 128;
     if (A.dout <= 64) return two ? run<Shape<4, 2, 4, 2>, KIND, E>(A, s) : run<Shape<4, 1, 4, 2>, KIND, E>(A, s);
     if (A.dout <= 128) return two ? run<Shape<8, 2, 4, 2>, KIND, E>(A, s) : run<Shape<8, 1, 4, 2>, KIND, E>(A, s);
-    if (A.dout <= 256) return two ? run<Shape<16, 2, 4, 2>, KIND, E>(A, s) : run<Shape<16, 1, 4, 2>, KIND, E>(A, s);
-    if (A.dout <= 384) return run<Shape<24, 1, 4, 2>, KIND, E>(A, s);
-    if (A.dout <= 512) return run<Shape<32, 1, 8, 1>, KIND, E>(A, s);
-    return run<Shape<16, 2, 4, 1>, KIND, E, true>(A, s);
+    if constexpr (KIND != kCbsr1) {  // (columns of a byte are below 256)
+        if (A.dout > 512) return run<Shape<16, 2, 4, 1>, KIND, E, true>(A, s);
+        if (A.dout > 384) return run<Shape<32, 1, 8, 1>, KIND, E>(A, s);
+        if (A.dout > 256) return run<Shape<24, 1, 4, 2>, KIND, E>(A, s);
+    }
+    return two ? run<Shape<16, 2, 4, 2>, KIND, E>(A, s) : run<Shape<16, 1, 4, 2>, KIND, E>(A, s);
 }
 
 }  // namespace
