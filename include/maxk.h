@@ -249,7 +249,8 @@ MAXK_API maxk_status spmm_baseline(maxk_graph* g, const float* d_H, int32_t dim,
  * Code arrays are 16-byte aligned.  Either format holds at most 8 significant bits, so its values are exact in bf16.
  * Beyond the conventions above: widths are at most MAXK_MX_MAX_DIM (MAXK_UNSUPPORTED), N below 2^31 - 15, and a gradient dH
  * comes dense (row-major [N x dout] of a MAXK_VALUE_* format) or, in the *_cbsr calls, as maxk_sspmm_bwd leaves it:
- * d_dXs fp32 [N x k] at the distinct columns sp_index [N x k] below dout, zeros elsewhere.  These calls need no maxk_graph, allocate
+ * d_dXs fp32 [N x k] at the distinct columns sp_index [N x k] below dout, zeros elsewhere.  The matrix products take an fp32 gradient in bf16
+ * parts that add up to it, but for its bits below 2^-133, which bf16 does not have: they are dropped.  These calls need no maxk_graph, allocate
  * nothing and may be captured into a HIP graph.  Products with a non-finite operand give non-finite sums, as they do in a
  * dense product (Inf may become NaN).
  */

@@ -1,7 +1,7 @@
 // Input gradient of the linear map with 4-bit weights (include/maxk.h): dX = dH W.
 //
 // On bf16 matrix instructions with fp32 accumulators.  W is exact in bf16, and a gradient is cut into bf16 parts that add up to it
-// exactly (fp32 three, fp16 two), so every product is exact and only the sums round.  A wavefront has 32 * IT columns of dX: it keeps those columns of W in
+// exactly (fp32 three, fp16 two; mx_parts.hpp), so every product is exact and only the sums round.  A wavefront has 32 * IT columns of dX: it keeps those columns of W in
 // its registers and walks over tiles of 32 rows of dH, which the four wavefronts of a group bring to LDS together: a CBSR gradient as its k values a
 // row, spread over zeros.  A workgroup has two groups; one fills its tile while the other multiplies.
 //

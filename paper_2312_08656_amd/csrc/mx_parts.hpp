@@ -1,4 +1,4 @@
-// What the gradient kernels of the microscaled operators share: bf16 matrix operands, and gradients cut into exact bf16 parts.
+// What the gradient kernels of the microscaled operators share: bf16 matrix operands, and gradients cut into bf16 parts.
 #pragma once
 
 #include <type_traits>
@@ -31,7 +31,8 @@ __device__ __forceinline__ uint32_t uppers(float low, float high)
 }
 __device__ __forceinline__ float upper_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 
-// x = sum of its parts, each of at most 8 significant bits (x of 24, 11 or 8)
+// x = sum of its parts, each of at most 8 significant bits (x of 24, 11 or 8).  Bits of x below 2^-133, the least that bf16 has, are dropped: an fp32 value of
+// 2^-110 or more has none, and a gradient that small is lost in any sum with one that is not.
 template <int P>
 __device__ __forceinline__ void split(float x, float* part)
 {

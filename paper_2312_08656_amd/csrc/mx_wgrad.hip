@@ -1,7 +1,7 @@
 // Weight gradient from a microscaled checkpoint (include/maxk.h): dW = dH^T X over N rows, and db.
 //
 // A product with few outputs and a long sum, on bf16 matrix instructions with fp32 accumulators.  X is exact in bf16 in either format.  An fp32
-// gradient is cut into three bf16 parts of 8 bits that add up to it exactly, fp16 into two: every product is exact, and only the
+// gradient is cut into three bf16 parts of 8 bits that add up to it exactly, fp16 into two (mx_parts.hpp): every product is exact, and only the
 // sums round, as in fp32.  A CBSR gradient is spread over a row of zeros in LDS, so it is read as k values and columns.
 //
 // Rows are cut into ranges.  A workgroup owns a tile of dW for a range; it has GR groups of wavefronts that take its steps of 32 rows in
