@@ -1880,7 +1880,7 @@ MAXK_API const char* maxk_status_string(maxk_status s)
         case MAXK_UNSUPPORTED: return "unsupported size";
         case MAXK_HIP_ERROR: return "HIP runtime error";
         case MAXK_OUT_OF_MEMORY: return "out of device or host memory";
-        case MAXK_SCRATCH_TOO_SMALL: return "the input needs more scratch memory than the library's fixed array holds";
+        case MAXK_SCRATCH_TOO_SMALL: return "more scratch memory is needed than the workspace given, or the library's fixed array, holds";
         default: return "unknown status";
     }
 }

@@ -13,3 +13,8 @@ def test_a_single_range_keeps_no_sums(din, dout):
 @pytest.mark.parametrize("din,dout", [(64, 64), (256, 256), (384, 384)])
 def test_ranges_keep_their_sums(din, dout):
     assert maxk.mx_weight_grad_workspace(232965, din, dout) >= 2 * 4 * dout * (din + 1)
+
+
+def test_too_small_a_workspace_is_named():
+    text = maxk.load_library().maxk_status_string(-5)
+    assert b"workspace" in text and b"scratch" in text
