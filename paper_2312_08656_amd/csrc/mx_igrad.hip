@@ -5,8 +5,9 @@
 // its registers and walks over tiles of 32 rows of dH, which the four wavefronts of a group bring to LDS together: a CBSR gradient as its k values a
 // row, spread over zeros.  A workgroup has two groups; one fills its tile while the other multiplies.
 //
-// Bound by the way to memory where dH is dense (169 thousand rows, 256 x 256, fp32: 58 us, 6.0 TB/s), by the three parts' products beside the stores of dX where
-// it is CBSR (233 thousand, k = 32: 64 us; the products alone 37 at the clock it runs at, the stores 43).
+// Bound by the way to memory where dH is dense (169 thousand rows, 256 x 256, fp32: 75 us, 4.6 TB/s, 59 to 65 with dH in the Infinity Cache; bf16 38, 4.5 TB/s; fp16 46), by the
+// three parts' products beside the stores of dX where it is CBSR (233 thousand, k = 32: 63 to 72 us by the card's clock; the products alone 37, the stores 43).  Dense rows that
+// are not whole 16-byte pieces come element by element: bf16 dH of 255 columns 150 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(S::THREADS) input_grad_kernel(const Args A)
         }
     } else {
         // A round's results leave while the next one's tile is filled: at the end of the products their way out would hold up the barrier, and the other
-        // group with it (932 thousand rows, 256 x 256, CBSR k = 32: 282 us there).
+        // group with it (932 thousand rows, 256 x 256, CBSR k = 32: 251 to 265 us, 282 there).
         const auto multiply_next = [&]() {
             load(t + stride, 0);
             local_fence();
@@ -348,6 +349,8 @@ maxk_status run(Args A, hipStream_t s)
     A.spans = (A.din + S::SPAN - 1) / S::SPAN;
     A.chunks = (A.dout + 16 * S::KC - 1) / (16 * S::KC);
     const int64_t tiles = (A.N + kRows - 1) / kRows;
+    // two workgroups a CU where W takes up to 8 operands a lane (most of those use up to 128 registers; CBSR of up to 64 columns at din above 128, and at k above 32, uses 130 to 160, and
+    // its 512 take two turns), else one
     A.slots = std::max<int64_t>(1, std::min((tiles + S::GR - 1) / S::GR, (int64_t)(S::KC * S::IT <= 8 ? 512 : 256) / A.spans));
     const int64_t grid = (A.slots + 7) / 8 * A.spans * 8;
     hipLaunchKernelGGL((input_grad_kernel<S, KIND, E, CHUNKED>), dim3((unsigned)grid), dim3(S::THREADS), 0, s, A);
@@ -359,8 +362,10 @@ template <int KIND, int E = 1>
 maxk_status run_kind(const Args& A, hipStream_t s)
 {
     // Four wavefronts hold 128 columns of dX, 32 each, or 256.  dH up to 256 columns leaves them the registers for two blocks of W each; up to 384 LDS holds two
-    // groups' tiles (200 thousand rows, CBSR k = 32, 384 -> 256 columns: 88 us, 162 as below); up to 512 one group of eight wavefronts fills and multiplies in turn
-    // (512 -> 384: 379 us); wider dH comes in chunks of 256 columns, and W anew with each.
+    // groups' tiles (200 thousand rows, CBSR k = 32, 384 -> 256 columns: 89 to 92 us, 162 as below); up to 512 one group of eight wavefronts fills and multiplies in turn
+    // (512 -> 384: 376 us); wider dH comes in chunks of 256 columns, and W anew with each (600 -> 256: 375 us).  Registers that are spilled to memory: with dH of 385 to 512 columns 14 to 49
+    // in CBSR forms, 1 to 36 in dense ones; with two blocks of W of 129 to 256 columns 1 to 4 at k above 32, and 12 to 29 in dense rows that come element by element, which spill 6 to 22 up
+    // to 384 columns; elsewhere none.
     const bool two = A.din > 128;
     if (A.dout <= 64) return two ? run<Shape<4, 2, 4, 2>, KIND, E>(A, s) : run<Shape<4, 1, 4, 2>, KIND, E>(A, s);
     if (A.dout <= 128) return two ? run<Shape<8, 2, 4, 2>, KIND, E>(A, s) : run<Shape<8, 1, 4, 2>, KIND, E>(A, s);

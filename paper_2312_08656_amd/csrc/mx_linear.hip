@@ -4,9 +4,10 @@
 // either operand.  Rows are many and widths small, so a wavefront keeps 64 rows of W (all their columns) in its registers and walks
 // over the rows of X, 16 at a time; the next 16 are on their way meanwhile.  Wavefronts that share rows of X lie in one workgroup, so X is read through L1.
 //
-// Bound by the way to memory, mostly Y's way out: 2.4 M rows, 256 to 256, fp32 Y 541 us (2.78 GB, 5.1 TB/s, what a large copy reaches); 1 M rows
-// 181 us (6.4 TB/s, X in the Infinity Cache); 1.1 M rows, 384 to 256, bf16 Y 147 us (5.3 TB/s).  One row, 256 to 256: 3.9 us a call, two round trips to memory
-// and the launch.
+// Bound by the way to memory, mostly Y's way out: 2.4 M rows, 256 to 256, fp32 Y 570 us (2.84 GB, 5.0 TB/s, what a large copy reaches); 1 M rows
+// 181 us with X in the Infinity Cache (6.4 TB/s), 259 without (4.5); 1.1 M rows, 384 to 256, bf16 Y 149 to 153 and 200 us.  One row, 256 to 256: 3.9 us a call, two round
+// trips to memory and the launch.  Farther from it: 16-bit Y (2.4 M rows, 256 to 256, bf16 420 us, the bytes 310; 256 to 100, whose rows leave a column a lane, 242 and 157) and
+// more than 512 columns in (1 M rows, 768 to 256, fp32 597 us and 341; 1433 to 256, whose Y leaves in pieces of 64 bytes, 1180 and 637).
 #include <algorithm>
 
 #include "mx_parts.hpp"
@@ -218,8 +219,10 @@ __global__ void __launch_bounds__(256) linear_long_kernel(MxMatrix X, int64_t N,
             }
 }
 
-// 3 for each of the 1024 SIMDs.  us at 2600 / 3 x 1024 / 3400 wavefronts, 2.4 M rows, 256 to 256: 656 / 554 / 665 (whole workgroups a CU are faster than odd ones),
-// at 2048 689.
+// 3 for each of the 1024 SIMDs.  us at 2048 / 2600 / 3 x 1024 / 3400 / 4096 wavefronts, 2.4 M rows, 256 to 256, fp32 Y: 677 / 662 / 570 / 671 / 612, 1 M rows 185 / 212 / 180 / 210 /
+// 197 (whole workgroups a CU are faster than odd ones).  One number for all instances, and not the best of each: bf16 Y, 2.4 M rows 504 / 490 / 420 / 408 / 317; 768 to 256
+// columns, where 256 registers a lane (18 more are spilled for fp32 Y) leave room for 2 a SIMD, 1 M rows 457 / 675 / 598 / 556 / 501; 256 to 320, five column
+// groups, 1.2 M rows 314 / 367 / 322 / 305 / 353.
 constexpr int64_t kWaves = 3 * 1024;
 
 template <int C, int VT>
@@ -229,8 +232,8 @@ void launch_chunks(const MxMatrix& X, int64_t N, const MxMatrix& W, int nb, int 
     const int64_t steps = (N + kTileRows * m - 1) / (kTileRows * m), blocks = std::min(steps, std::max<int64_t>(1, kWaves / (gcols * m * sides)));
     const size_t lds = 2 * sizeof(float) * (size_t)(kTileRows * m) * (gcols * kGroup + kPad);
     // Where X does not stay in the Infinity Cache its reads share the way to memory with Y's writes, and do better if a step waits for the writes of the
-    // one before.  us, with / without: 2.4 M rows, 256 to 256 541 / 617, bf16 Y 395 / 405; 1.2 M, 512 to 384 612 / 593; below that size 1.6 M, 256 to 256 304 / 300,
-    // 0.1 M 22.1 / 21.2.
+    // one before.  us, with / without: 2.4 M rows, 256 to 256 569 / 626, bf16 Y 421 / 407; 1.2 M, 512 to 384 615 / 594; below that size 1.6 M, 256 to 256 303 / 293,
+    // 0.1 M 21.9 / 20.9.
     const bool pace = (double)N * nb * 17 > kInfinityCache;
     const dim3 grid((unsigned)blocks, (unsigned)sides), block(64 * gcols * m);
 #define MAXK_LINEAR(WIDE, ONCE) hipLaunchKernelGGL((linear_kernel<C, VT, WIDE, ONCE>), grid, block, lds, s, X, N, W, nb, dout, gcols, m, pace, bias, Y)

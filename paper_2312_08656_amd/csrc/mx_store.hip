@@ -2,8 +2,9 @@
 //
 // Both directions are streams: what they read and write once is all they cost.  A lane takes a unit of 8 columns, four lanes a
 // block: 16-byte loads or stores on the side of X, 8 or 4 bytes of codes, and the largest magnitude of a block is two DPP steps away.
-// A thread has kUnits units under way, a workgroup's width apart.  717 thousand rows of 384 bf16 to 8 bits 127 us (6.5 TB/s), back 147 (5.7); a large copy
-// reaches 5.1 TB/s.
+// A thread has kUnits units under way, a workgroup's width apart.  717 thousand rows of 384 bf16 to 8 bits 125 to 131 us (6.5 TB/s), back 143 to 150 (5.7); a large copy
+// reaches 5.1 TB/s.  Rows that are not whole 16-byte pieces go element by element, bound by the number of accesses: 2.4 M rows of 100 bf16, to 8 bits and back, 722 us
+// where the bytes would take 311.
 #include "mx.hpp"
 
 namespace maxk {

@@ -8,10 +8,11 @@
 // turn, each with its own tiles of X and dH in LDS, and adds the groups' sums up in LDS at the end.  With two groups one fills its tiles while the other
 // multiplies.  The ranges' sums go to the workspace and a second kernel adds them up, always in the same order.
 //
-// What it takes, 233 thousand rows, 256 x 256, CBSR k = 32: 82 us, of which 7 are the second kernel and 15 the start, the joining of groups and 32 MB of sums on
-// their way out; the rounds run at 60 % of what the three parts' products alone would (bound by the barriers between two groups that take turns, and by
-// LDS, half of its cycles busy).  Without db 80, without bringing dH and X 54 and those 22.  2.4 M rows, 64 x 64, dense fp32: 161 us (4.8 TB/s, memory); 717 thousand,
-// 384 x 384, bf16 from 4 bits: 281 us (2.5 TB/s; a phase of products is short against the way to memory, and the registers hold one round's values).
+// What it takes, 233 thousand rows, 256 x 256, CBSR k = 32: 84 to 90 us by the card's clock, of which 7 are the second kernel and 15 the start, the joining of groups and 32 MB
+// of sums on their way out; the rounds run at 60 % of what the three parts' products alone would (bound by the barriers between two groups that take turns; matrix
+// units 44 % busy, LDS a third).  Where it took 82: without db 80, without bringing dH and X 54 and those 22.  2.4 M rows, 64 x 64, dense fp32: 158 us (4.9 TB/s, memory);
+// 717 thousand, 384 x 384, from 4 bits: bf16 281 to 303 us (2.4 TB/s; a phase of products is short against the way to memory, and the registers hold one round's values),
+// fp16 484 to 503 (two parts).
 #include <algorithm>
 #include <type_traits>
 
@@ -439,11 +440,14 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
     p.otiles = (dout + S::TO - 1) / S::TO;
     p.itiles = (din + S::TI - 1) / S::TI;
     const int64_t tiles = (int64_t)p.otiles * p.itiles, steps = (N + kStep - 1) / kStep;
-    const int64_t resident = S::ACC > 64 ? 256 : 512, rounds = (steps + S::GR - 1) / S::GR;  // workgroups that run at a time; rounds of a single range
+    // Workgroups that ranges are made for: one a CU, or two where a lane has 64 accumulators.  Two run at a time for aligned bf16 gradients as Middle alone; elsewhere LDS (Small)
+    // or registers (Middle) leave room for one, and 512 take two turns.  us at 512 / 256: 717 thousand rows, 384 x 384, bf16 286 / 400; 200 thousand, fp32, 384 x 384 209 / 220,
+    // 256 x 384 152 / 146; 2.4 M, 64 x 64, fp32 158 / 145, bf16 97 / 90, CBSR k = 8 105 / 95; 500 thousand, 100 x 100, k = 13 73 / 65.
+    const int64_t resident = S::ACC > 64 ? 256 : 512, rounds = (steps + S::GR - 1) / S::GR;  // rounds of a single range
     // A round takes about 2 us, the second kernel 3 and more with more ranges: one range up to two rounds, a range each up to 32, then two rounds a range
-    // until no more workgroups run at a time.  (us, 256 x 256, CBSR k = 32: 256 rows 18.1 as one range / 12.2 as four; 4000 rows 19.8 as 31 / 21.3 as 63;
-    // 64 x 64, 1024 rows, k = 8: 15.7 as one / 10.4 as four.)
-    // Every XCD has an eighth of the ranges, and of the workgroups that run: one range more than it has room for would take it twice as long (384 x 384: 6 tiles).
+    // until there are as many workgroups.  (us, 256 x 256 as Wide, CBSR k = 32: 256 rows 18.2 as one range / 12.5 as four; 4000 rows 19.8 as 31 / 21.7 as 63;
+    // 64 x 64, 1024 rows, k = 8: 15.9 as one / 10.6 as four.)
+    // Every XCD has an eighth of the ranges, and of the workgroups: one range more would take it another turn (384 x 384: 6 tiles).
     const int64_t most = tiles <= resident / 8 ? resident / 8 / tiles * 8 : std::max<int64_t>(1, resident / tiles);
     p.ranges = rounds <= 2 ? 1 : std::min(most, std::max(std::min<int64_t>(rounds, 32), rounds / 2));
     p.sums = p.ranges > 1 ? p.ranges * tiles * S::TILE : 0;
@@ -451,13 +455,13 @@ Plan plan_of(int shape, int64_t N, int din, int dout)
     return p;
 }
 
-// us, 200 thousand rows, as Middle / Wide: CBSR k = 8, 64 x 384 83 / 74, 256 x 384 155 / 129, 384 x 384 213 / 197, k = 64 107 / 80, 205 / 141, 283 / 215 (every tile
-// of dH looks at all entries of its rows); dense fp32 85 / 91, 147 / 165, 204 / 237, bf16 256 x 384 65 / 77.
+// us, 200 thousand rows, din x dout, as Middle / Wide: CBSR k = 8, 64 x 384 83 / 74, 256 x 384 154 / 127, 384 x 384 212 / 195, k = 64 108 / 80, 207 / 141, 286 / 215 (every tile
+// of dH looks at all entries of its rows); dense fp32 86 / 92, 152 / 165, 209 / 242, bf16 256 x 384 65 / 77; fp32 384 x 256, whose columns of dH fill Wide, 151 / 133.
 Plan plan(int64_t N, int din, int dout, bool cbsr)
 {
-    // Few rows: small tiles, as long as all of them have a workgroup for every round, with eight groups a round.  us as above / so, CBSR k = 16: 256 x 256, 100 rows 13.4 /
-    // 8.9, 4000 18.2 / 13.6; 384 x 384, 1000 rows 19.8 / 12.7, 8000 30.7 / 34.4; 64 x 256, 8000 rows 19.5 / 11.7.  One tile of Middle is its equal up to 4000 rows
-    // (100 x 100: 500 rows 9.7 / 11.9, 8000 15.0 / 11.7).  Dense fp32: 256 x 256, 100 rows 12.7 / 8.0, 4000 17.9 / 12.7; 384 x 384, 1000 rows 14.9 / 11.3.
+    // Few rows: small tiles, as long as 512 workgroups give all of them one for every round, with eight groups a round (256 run at a time).  us as above / so, CBSR k = 16: 256 x 256,
+    // 100 rows 13.5 / 8.8, 4000 18.2 / 13.5; 384 x 384, 1000 rows 19.9 / 12.6, 8000 30.9 / 34.5; 64 x 256, 8000 rows 19.5 / 11.6.  One tile of Middle is its equal up to 4000 rows
+    // (100 x 100: 500 rows 9.8 / 12.0, 8000 15.0 / 11.6).  Dense fp32: 256 x 256, 100 rows 12.7 / 8.0, 4000 17.9 / 12.6; 384 x 384, 1000 rows 14.8 / 11.5.
     const int64_t steps = (N + kStep - 1) / kStep, tiles = (int64_t)((din + 63) / 64) * ((dout + 63) / 64);
     const bool few = (steps + Small::GR - 1) / Small::GR * tiles <= 512 && (din > 128 || dout > 128 || steps > 128);
     if (few || (din <= 64 && dout <= 64)) return plan_of<Small>(0, N, din, dout);
@@ -479,7 +483,7 @@ template <class S>
 maxk_status run_shape(const Args& A, int format, hipStream_t s)
 {
     maxk_status st;
-    constexpr int WIDEST = S::TO == 128 ? 16 : 8;  // (16 would not fit Wide's registers, and Small's rows are few or have k up to 64)
+    constexpr int WIDEST = S::TO == 128 ? 16 : 8;  // (16 would not fit Wide's registers, and Small's rows are few or have k up to 64; of 8, Small spills 2 to 4 registers at two-byte columns)
     const bool pieces = aligned(A.G.values, 16) && A.dout * (A.G.value_type == MAXK_VALUE_F32 ? 4 : 2) % 16 == 0;  // rows of whole 16-byte pieces
 #define MAXK_ENTRIES(KIND)                                                                                                                            \
     st = A.G.k <= 32   ? (format == MAXK_MX_8 ? run<S, MAXK_MX_8, KIND, 4>(A, s) : run<S, MAXK_MX_4, KIND, 4>(A, s))                                  \
