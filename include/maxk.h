@@ -299,6 +299,83 @@ MAXK_API maxk_status maxk_mx_input_grad_cbsr(const float* d_dXs, const void* d_s
                                              const uint8_t* d_w_codes, const uint8_t* d_w_scales, int32_t din, int32_t dout, void* d_dX,
                                              int32_t dx_value_type, void* stream);
 
+/*
+ * The same product for few rows of X that are not rounded: Y[n,o] = bias[o] + sum_i X[n,i] W[o,i], X [N x din] in a MAXK_VALUE_* format, W [dout x din]
+ * MAXK_MX_4, fp32 sums, Y [N x dout] in a MAXK_VALUE_* format of its own (rounded once).  16 rows cost about what one does; 17 to
+ * MAXK_MX_MATVEC_MAX_ROWS read W again for every 16 (more: MAXK_UNSUPPORTED).  dout is at most MAXK_MAX_CLASSES.  Of an fp32 X the bits below 2^-133 are
+ * dropped.  Codes behind column din have to be those of zero, as maxk_mx_quantize leaves them.
+ */
+#define MAXK_MX_MATVEC_MAX_ROWS 1024
+MAXK_API maxk_status maxk_mx_matvec(const void* d_X, int32_t value_type, int64_t N, const uint8_t* d_w_codes, const uint8_t* d_w_scales, int32_t din,
+                                    int32_t dout, const float* d_bias, void* d_Y, int32_t y_value_type, void* stream);
+
+/*
+ * Both ends of a classifier: the norm in front of a layer, and log probabilities and a teacher's loss behind the last one.  Matrices are row-major in a
+ * MAXK_VALUE_* format and aligned to its elements, N is below 2^31 - 15; sums are fp32 or wider, and the same call gives the same bits.  These calls need
+ * no maxk_graph, allocate nothing and may be captured into a HIP graph; a workspace (16-byte aligned) may be used again by later work on the
+ * stream.  MAXK_SCRATCH_TOO_SMALL where workspace_bytes is less than a call needs.
+ *
+ * Root-mean-square norm with the residual's addition:  H = X + residual (rounded to the format), r = 1 / sqrt(mean of a row's H^2 + eps),
+ * Y[n,i] = H[n,i] r[n] gamma[i], of X [N x dim], gamma fp32 [dim], eps positive and finite.  d_residual and d_H are both given or both NULL (H is X then);
+ * H may be X's or the residual's own memory.  Y leaves in X's format (d_Y; X's or the residual's memory too, where H is not there), in `format` as
+ * maxk_mx_quantize would store its fp32 value (d_codes, d_scales), or both.  d_rstd (fp32 [N], r for the gradient) may be NULL.  dim is at most
+ * MAXK_NORM_MAX_DIM.
+ */
+#define MAXK_NORM_MAX_DIM 16384
+MAXK_API maxk_status maxk_rms_norm(const void* d_X, const void* d_residual, int32_t value_type, int64_t N, int32_t dim, const float* d_gamma, double eps,
+                                   void* d_H, void* d_Y, int32_t format, void* d_codes, uint8_t* d_scales, float* d_rstd, void* stream);
+
+/*
+ * Its gradients, for the H and r of the call:  with x = H r and g = dY gamma,  dX = r (g - x mean of a row's g x) + dH,  the gradient of X and of
+ * the residual alike (d_dH, the gradient that arrives at H, may be NULL: zero), and dgamma[i] = sum_n dY[n,i] x[n,i], fp32 [dim] (NULL: not computed).  dX
+ * may be the memory of dY or dH.  For dgamma d_workspace holds maxk_rms_norm_grad_workspace(N, dim) bytes (never 0).
+ */
+MAXK_API int64_t maxk_rms_norm_grad_workspace(int64_t N, int32_t dim);
+MAXK_API maxk_status maxk_rms_norm_grad(const void* d_dY, const void* d_H, const void* d_dH, int32_t value_type, int64_t N, int32_t dim,
+                                        const float* d_gamma, const float* d_rstd, void* d_dX, float* d_dgamma, void* d_workspace,
+                                        int64_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities:  log p = x - log(sum exp x) of a row x of logits [N x V], V at most MAXK_MAX_CLASSES.
+ *   d_logprob  fp32 [N]      log p of the row's given class, d_labels int32 or int64 (label_bytes 4 or 8) [N].  A negative label is no class: 0.  One from V on: NaN.
+ *   d_entropy  fp32 [N]      -sum p log p, 0 log 0 being 0
+ *   d_top_data, d_top_index  the k likeliest classes, fp32 [N x k] log probabilities and their columns [N x k] in index_bytes (as sp_index), likeliest first,
+ *                            the lower column first among equals; k from 1 to MAXK_MAX_ALTERNATIVES and V, or 0 with both NULL
+ * Any of them may be NULL, not all.  A logit of -Inf is a class that is masked out.  A row in which nothing is left has log probabilities of -Inf and entropy
+ * 0, one with a NaN or +Inf gives NaN (and columns within the row).  d_workspace holds maxk_classes_workspace(N, V, k) bytes, which may be 0 (d_workspace
+ * may then be NULL).
+ *
+ * The gradient of sum_n dlogprob[n] logprob[n] + dentropy[n] entropy[n], either vector fp32 [N] or NULL, not both: dlogits [N x V] in the logits' format, whose
+ * memory it may be.  A row without a class has no gradient from dlogprob, one in which nothing is left none at all; a label from V on makes its row NaN.
+ * logprob and entropy (NULL: not wanted) are those of maxk_logprobs, so that a training step whose dlogprob and dentropy are known is this one call.  Workspace: k = 0.
+ */
+#define MAXK_MAX_CLASSES (1 << 24)
+#define MAXK_MAX_ALTERNATIVES 64
+MAXK_API int64_t maxk_classes_workspace(int64_t N, int32_t V, int32_t k);
+MAXK_API maxk_status maxk_logprobs(const void* d_logits, int32_t value_type, int64_t N, int32_t V, const void* d_labels, int32_t label_bytes,
+                                   float* d_logprob, float* d_entropy, float* d_top_data, void* d_top_index, int32_t index_bytes, int32_t k,
+                                   void* d_workspace, int64_t workspace_bytes, void* stream);
+MAXK_API maxk_status maxk_logprobs_grad(const void* d_logits, int32_t value_type, int64_t N, int32_t V, const void* d_labels, int32_t label_bytes,
+                                        const float* d_dlogprob, const float* d_dentropy, float* d_logprob, float* d_entropy, void* d_dlogits,
+                                        void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Distillation from a teacher's largest logits, k a row in any order: d_top_data [N x k] in a format of its own at the columns d_top_index [N x k]
+ * (index_bytes as sp_index).  With q = softmax over a row's entries of data / temperature and p = softmax(logits / temperature) over all V classes
+ *   loss[n] = sum_t q_t (log q_t - log p[index_t]),   dlogits[n,j] = dloss[n] / temperature (p_j - sum of q_t over the entries of column j).
+ * An entry of -Inf, or whose column lies outside [0, V), is none; entries of one column each count.  A row without entries has loss 0 and no gradient; one whose logits
+ * are all -Inf loss +Inf (0 without entries) and no gradient; q > 0 at a logit of -Inf gives loss +Inf and the formula's gradient.  maxk_distill_grad writes the loss too where d_loss
+ * is given; dlogits may be the logits' own memory.  k is at most MAXK_DISTILL_MAX_K; temperature positive, it and its reciprocal within fp32's range.
+ * Workspace: maxk_classes_workspace(N, V, 0).
+ */
+#define MAXK_DISTILL_MAX_K 1024
+MAXK_API maxk_status maxk_distill(const void* d_logits, int32_t value_type, int64_t N, int32_t V, const void* d_top_data, int32_t top_value_type,
+                                  const void* d_top_index, int32_t index_bytes, int32_t k, double temperature, float* d_loss, void* d_workspace,
+                                  int64_t workspace_bytes, void* stream);
+MAXK_API maxk_status maxk_distill_grad(const void* d_logits, int32_t value_type, int64_t N, int32_t V, const void* d_top_data, int32_t top_value_type,
+                                       const void* d_top_index, int32_t index_bytes, int32_t k, double temperature, const float* d_dloss, float* d_loss,
+                                       void* d_dlogits, void* d_workspace, int64_t workspace_bytes, void* stream);
+
 /* Text for a status code (static storage). */
 MAXK_API const char* maxk_status_string(maxk_status s);
 

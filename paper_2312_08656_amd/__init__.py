@@ -40,11 +40,22 @@ from .mx import (  # noqa: E402,F401
     maxk_mx_input_grad,
     maxk_mx_input_grad_cbsr,
     maxk_mx_linear,
+    maxk_mx_matvec,
     maxk_mx_quantize,
     maxk_mx_weight_grad,
     maxk_mx_weight_grad_cbsr,
     mx_blocks,
     mx_empty,
     mx_weight_grad_workspace,
+)
+from .heads import (  # noqa: E402,F401
+    classes_workspace,
+    maxk_distill,
+    maxk_distill_grad,
+    maxk_logprobs,
+    maxk_logprobs_grad,
+    maxk_rms_norm,
+    maxk_rms_norm_grad,
+    rms_norm_grad_workspace,
 )
 from .autograd import MaxKAggregate, MaxKLayer, maxk_aggregate, maxk_layer  # noqa: E402,F401

@@ -27,7 +27,9 @@ EXPORTS = (
     "maxk_graph_limit_allocations", "maxk_expand_past_l2", "maxk_scatter_past_l2", "maxk_lone_visit_line",
     "maxk_entry_batch", "maxk_fwd_by_units", "maxk_pull_by_units",
     "maxk_mx_quantize", "maxk_mx_dequantize", "maxk_mx_linear", "maxk_mx_weight_grad_workspace", "maxk_mx_weight_grad",
-    "maxk_mx_weight_grad_cbsr", "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr",
+    "maxk_mx_weight_grad_cbsr", "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr", "maxk_mx_matvec",
+    "maxk_rms_norm", "maxk_rms_norm_grad_workspace", "maxk_rms_norm_grad", "maxk_classes_workspace", "maxk_logprobs", "maxk_logprobs_grad",
+    "maxk_distill", "maxk_distill_grad",
 )
 
 
@@ -112,8 +114,21 @@ def load_library() -> ctypes.CDLL:
     lib.maxk_mx_weight_grad_cbsr.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, i32, i32, vp, vp, vp, i64, vp]
     lib.maxk_mx_input_grad.argtypes = [vp, i32, i64, vp, vp, i32, i32, vp, i32, vp]
     lib.maxk_mx_input_grad_cbsr.argtypes = [vp, vp, i32, i32, i64, vp, vp, i32, i32, vp, i32, vp]
+    lib.maxk_mx_matvec.argtypes = [vp, i32, i64, vp, vp, i32, i32, vp, vp, i32, vp]
+    f64 = ctypes.c_double
+    lib.maxk_rms_norm.argtypes = [vp, vp, i32, i64, i32, vp, f64, vp, vp, i32, vp, vp, vp, vp]
+    lib.maxk_rms_norm_grad_workspace.argtypes = [i64, i32]
+    lib.maxk_rms_norm_grad_workspace.restype = i64
+    lib.maxk_rms_norm_grad.argtypes = [vp, vp, vp, i32, i64, i32, vp, vp, vp, vp, vp, i64, vp]
+    lib.maxk_classes_workspace.argtypes = [i64, i32, i32]
+    lib.maxk_classes_workspace.restype = i64
+    lib.maxk_logprobs.argtypes = [vp, i32, i64, i32, vp, i32, vp, vp, vp, vp, i32, i32, vp, i64, vp]
+    lib.maxk_logprobs_grad.argtypes = [vp, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.maxk_distill.argtypes = [vp, i32, i64, i32, vp, i32, vp, i32, i32, f64, vp, vp, i64, vp]
+    lib.maxk_distill_grad.argtypes = [vp, i32, i64, i32, vp, i32, vp, i32, i32, f64, vp, vp, vp, vp, i64, vp]
     for name in ("maxk_mx_quantize", "maxk_mx_dequantize", "maxk_mx_linear", "maxk_mx_weight_grad", "maxk_mx_weight_grad_cbsr",
-                 "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr"):
+                 "maxk_mx_input_grad", "maxk_mx_input_grad_cbsr", "maxk_mx_matvec", "maxk_rms_norm", "maxk_rms_norm_grad", "maxk_logprobs",
+                 "maxk_logprobs_grad", "maxk_distill", "maxk_distill_grad"):
         getattr(lib, name).restype = i32
     lib.maxk_last_hip_error.argtypes = []
     lib.maxk_version.argtypes = []
@@ -131,7 +146,9 @@ def _load_fast(lib: ctypes.CDLL) -> None:
     _torch_calls.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.maxk_topk_cbsr_narrow, lib.maxk_spgemm_fwd_narrow, lib.maxk_spgemm_fwd_noalloc, lib.maxk_sspmm_bwd_narrow,
         lib.maxk_cbsr_scatter, lib.maxk_mx_quantize, lib.maxk_mx_dequantize, lib.maxk_mx_linear, lib.maxk_mx_weight_grad_workspace,
-        lib.maxk_mx_weight_grad, lib.maxk_mx_weight_grad_cbsr, lib.maxk_mx_input_grad, lib.maxk_mx_input_grad_cbsr)], _check)
+        lib.maxk_mx_weight_grad, lib.maxk_mx_weight_grad_cbsr, lib.maxk_mx_input_grad, lib.maxk_mx_input_grad_cbsr, lib.maxk_mx_matvec,
+        lib.maxk_rms_norm, lib.maxk_rms_norm_grad_workspace, lib.maxk_rms_norm_grad, lib.maxk_classes_workspace, lib.maxk_logprobs,
+        lib.maxk_logprobs_grad, lib.maxk_distill, lib.maxk_distill_grad)], _check)
     _FAST = _torch_calls
 
 
@@ -154,6 +171,14 @@ def _dev(t: torch.Tensor, dtype, what: str) -> int:
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
         raise MaxKError(f"{what}: expected a contiguous device tensor of {dtype}")
     return t.data_ptr()
+
+
+def _here(what: str, *tensors) -> None:
+    """Refuses tensors of another device than the current one, whose stream the call takes."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise MaxKError(f"{what}: expected tensors of the current device")
 
 
 def index_dtype(index_bytes: int):

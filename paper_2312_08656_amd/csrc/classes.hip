@@ -1,0 +1,570 @@
+// Log probabilities of classes and distillation from a teacher's largest logits (include/maxk.h), over rows of logits of any width.
+//
+//   m = max x,  d = (x - m) scale log2 e,  S = sum 2^d,  T = sum 2^d d:   log p = ln 2 d - ln S,   H = ln S - ln 2 T / S
+//   log probabilities:  dx = p (-g - u (log p + H)), + g at the given class
+//   distillation:       q = softmax(scale t) of the teacher's entries;  loss = sum q (log q - log p);  dx = g scale (p - sum of q at the column)
+//
+// One pass over a row has its maximum and sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end.  The gradient
+// reads the row again, from the caches, and writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.
+#include "heads.hpp"
+#include "rows.hpp"
+
+namespace maxk {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kFar = 256.f;  // 2^-256 is 0 in fp32: a difference past it need not be told, and is cut so that 0 times it stays 0
+
+// Of a part of a row: its largest value (the lowest fp32 value where it has none above), S and T.  -Inf adds 0, NaN and +Inf make S a NaN.
+struct Sums { float m, S, T; };
+__device__ __forceinline__ Sums no_sums() { return {-3.402823466e38f, 0.f, 0.f}; }
+
+__device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2f(d); }
+
+__device__ __forceinline__ void move_to(Sums& a, float m, float c)  // m at least a.m
+{
+    const float shift = fminf((m - a.m) * c, kFar), f = exp2_of(-shift);
+    a.T = f * fmaf(-shift, a.S, a.T);
+    a.S *= f;
+    a.m = m;
+}
+
+__device__ __forceinline__ float largest(const float (&x)[kRowUnit])
+{
+    float m = fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int j = 2; j < kRowUnit; ++j) m = fmaxf(m, x[j]);
+    return m;
+}
+
+__device__ __forceinline__ void absorb(Sums& a, const float (&x)[kRowUnit], float top, float c)
+{
+    move_to(a, fmaxf(a.m, top), c);
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) {
+        const float d = (x[j] - a.m) * c, e = exp2_of(d);
+        a.S += e;
+        a.T = fmaf(e, fmaxf(d, -kFar), a.T);
+    }
+}
+
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    move_to(a, m, c);
+    move_to(b, m, c);
+    return {m, a.S + b.S, a.T + b.T};
+}
+
+template <int L>
+__device__ __forceinline__ Sums join_lanes(Sums a, float c)
+{
+    const auto with = [&](auto step) {
+        constexpr int K = decltype(step)::value;
+        a = join(a, Sums{other_lane<K>(a.m), other_lane<K>(a.S), other_lane<K>(a.T)}, c);
+    };
+    if constexpr (L > 1) with(std::integral_constant<int, 1>{});
+    if constexpr (L > 2) with(std::integral_constant<int, 2>{});
+    if constexpr (L > 4) with(std::integral_constant<int, 4>{});
+    if constexpr (L > 8) with(std::integral_constant<int, 8>{});
+    if constexpr (L > 16) with(std::integral_constant<int, 16>{});
+    if constexpr (L > 32) with(std::integral_constant<int, 32>{});
+    return a;
+}
+
+__device__ __forceinline__ Sums join_workgroup(Sums a, float c, Sums* room)  // (passes a barrier, room is free behind the next one)
+{
+    a = join_lanes<kWave>(a, c);
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = a;
+    __syncthreads();
+    a = room[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) a = join(a, room[i], c);
+    return a;
+}
+
+// ---- the likeliest classes: keys are in the order of (value, lower column first) ----
+
+__device__ __forceinline__ uint32_t value_key(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.f);  // -0 is +0
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t col) { return (uint64_t)value_key(x) << 32 | (0xFFFFFFFFu - col); }
+
+__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
+{
+    return (uint64_t)(uint32_t)__shfl((int)(k >> 32), lane) << 32 | (uint32_t)__shfl((int)(uint32_t)k, lane);
+}
+__device__ __forceinline__ uint64_t greater_key(uint64_t a, uint64_t b) { return a > b ? a : b; }
+
+__device__ __forceinline__ uint64_t exchange(uint64_t k, int lane, int step, bool falling)
+{
+    const uint64_t o = lane_key(k, lane ^ step);
+    return (((lane & step) == 0) == falling) == (k > o) ? k : o;
+}
+// keys of the 64 lanes in falling order (equal ones only where both are 0)
+__device__ __forceinline__ uint64_t sort_keys(uint64_t k, int lane)
+{
+#pragma unroll
+    for (int size = 2; size <= kWave; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step > 0; step /= 2) k = exchange(k, lane, step, (lane & size) == 0);
+    return k;
+}
+// the 64 greatest of two sets in falling order, in falling order
+__device__ __forceinline__ uint64_t merge_keys(uint64_t a, uint64_t b, int lane)
+{
+    uint64_t k = greater_key(a, lane_key(b, 63 - lane));
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) k = exchange(k, lane, step, true);
+    return k;
+}
+
+// A wavefront's greatest keys: in falling order over the lanes, and those that wait in LDS to be sorted in.  A unit whose largest value is below the k-th
+// greatest key costs a comparison.
+struct Likeliest {
+    uint64_t mine, least;   // least: of a key that is still wanted (it is greater)
+    float least_value;
+    uint64_t* wait;         // 128 keys
+    int waiting, k, lane;
+
+    __device__ __forceinline__ void begin(int k_, uint64_t* wait_, int lane_)
+    {
+        mine = least = 0;
+        least_value = -__builtin_inff();
+        wait = wait_;
+        waiting = 0;
+        k = k_;
+        lane = lane_;
+    }
+    __device__ __forceinline__ void raise(uint64_t key)
+    {
+        least = key > least ? key : least;
+        least_value = least >> 32 ? key_value((uint32_t)(least >> 32)) : -__builtin_inff();
+    }
+    __device__ void sort_in()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int n = min(waiting, kWave), from = waiting - n;
+        const uint64_t key = lane < n ? wait[from + lane] : 0;
+        waiting = from;
+        mine = merge_keys(mine, sort_keys(key, lane), lane);
+        raise(lane_key(mine, k - 1));
+    }
+    // a unit at column `col`: all lanes come here, those without columns with valid < 1
+    __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid, bool first)
+    {
+        if (first) raise((uint64_t)(uint32_t)(lane_key(sort_keys((uint64_t)(valid > 0 ? value_key(top) : 0u) << 32, lane), k - 1) >> 32) << 32);
+        if (!__any(valid > 0 && top >= least_value)) return;
+#pragma unroll 1
+        for (int j = 0; j < kRowUnit; ++j) {
+            float v = x[0];
+#pragma unroll
+            for (int i = 1; i < kRowUnit; ++i) v = i == j ? x[i] : v;
+            const uint64_t key = key_of(v, (uint32_t)(col + j));
+            const bool wanted = j < valid && key > least;
+            const uint64_t who = __ballot(wanted);
+            if (!who) continue;
+            if (wanted) wait[waiting + __popcll(who & ((1ull << lane) - 1))] = key;
+            waiting += __popcll(who);
+            while (waiting >= kWave) sort_in();
+        }
+    }
+    __device__ __forceinline__ void end() { while (waiting > 0) sort_in(); }
+};
+
+// ---- a row ----
+
+__device__ __forceinline__ int64_t label_of(const ClassCall& C, int64_t row)
+{
+    return C.label_bytes == 8 ? ((const int64_t*)C.labels)[row] : (int64_t)((const int32_t*)C.labels)[row];
+}
+__device__ __forceinline__ int64_t column_of(const ClassCall& C, int64_t at)
+{
+    return C.index_bytes == 1 ? ((const uint8_t*)C.index)[at] : C.index_bytes == 2 ? ((const uint16_t*)C.index)[at] : ((const int32_t*)C.index)[at];
+}
+__device__ __forceinline__ float teacher_value(const ClassCall& C, int64_t at)
+{
+    if (C.data_type == MAXK_VALUE_F32) return ((const float*)C.data)[at];
+    const uint16_t v = ((const uint16_t*)C.data)[at];
+    return C.data_type == MAXK_VALUE_BF16 ? widen_value<MAXK_VALUE_BF16>(v) : widen_value<MAXK_VALUE_F16>(v);
+}
+
+// What a row asks of its columns beside S: log probabilities: x at the given class (x), whether there is one; distillation: the teacher's part.
+// loss = C + Q (ln S + (m - ref) scale) with C = sum q (log q - (x - ref) scale) over the teacher's entries, ref the largest x among them
+struct Asked { float x, C, ref, Q; };
+
+constexpr int kMostEntries = MAXK_DISTILL_MAX_K;
+struct Entries {  // of the teacher, in LDS
+    int32_t col[kMostEntries];
+    float q[kMostEntries], x[kMostEntries];
+};
+
+// max and sum over a workgroup (two barriers)
+__device__ __forceinline__ float workgroup_max(float x, float* room)
+{
+    x = over_lanes<kWave>(x, [](float a, float b) { return fmaxf(a, b); });
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
+    __syncthreads();
+    x = room[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) x = fmaxf(x, room[i]);
+    return x;
+}
+__device__ __forceinline__ float workgroup_sum(float x, float* room)
+{
+    x = over_lanes<kWave>(x, kAdd);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
+    __syncthreads();
+    x = room[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) x += room[i];
+    return x;
+}
+
+// The teacher's entries of a row, their q and the student's x there.  An entry whose column lies outside the row is none.
+template <int VT>
+__device__ Asked take_entries(const ClassCall& C, int64_t row, Entries& E, float* room)
+{
+    const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
+    float top = -3.402823466e38f, ref = -3.402823466e38f;
+    for (int i = threadIdx.x; i < C.k; i += kThreads) {
+        const int64_t col = column_of(C, row * C.k + i);
+        const bool there = col >= 0 && col < C.V;
+        E.col[i] = there ? (int32_t)col : -1;
+        E.q[i] = there ? teacher_value(C, row * C.k + i) : -__builtin_inff();
+        E.x[i] = there ? widen_value<VT>(x[col]) : -__builtin_inff();
+        top = fmaxf(top, E.q[i]);
+        ref = fmaxf(ref, E.x[i]);
+    }
+    top = workgroup_max(top, room);
+    ref = workgroup_max(ref, room);
+    const float c = C.scale * kLog2e;
+    float sum = 0.f;
+    for (int i = threadIdx.x; i < C.k; i += kThreads) sum += exp2_of((E.q[i] - top) * c);
+    sum = workgroup_sum(sum, room);
+    const float ln = logf(sum), inverse = 1.f / sum;
+    float loss = 0.f;
+    for (int i = threadIdx.x; i < C.k; i += kThreads) {
+        const float d = (E.q[i] - top) * c, q = sum == 0.f ? 0.f : exp2_of(d) * inverse;
+        if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - (E.x[i] - ref) * C.scale);
+        E.q[i] = q;
+    }
+    loss = workgroup_sum(loss, room);
+    return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
+}
+
+template <int VT>
+__device__ __forceinline__ Asked given_class(const ClassCall& C, int64_t row)
+{
+    const int64_t y = C.labels ? label_of(C, row) : -1;
+    return {y >= 0 && y < C.V ? widen_value<VT>(((const value_store_t<VT>*)C.logits)[row * C.V + y]) : 0.f, 0.f, 0.f, 0.f};
+}
+
+struct Found { float ln, logprob, entropy, loss; };  // of a whole row; ln = ln S
+
+__device__ __forceinline__ Found row_results(const ClassCall& C, int64_t row, const Sums& s, const Asked& a)
+{
+    Found f = {logf(s.S), 0.f, 0.f, 0.f};
+    if (C.index) {
+        f.loss = a.Q == 0.f ? 0.f : s.S == 0.f ? __builtin_inff() : a.C + a.Q * (f.ln + (s.m - a.ref) * C.scale);
+        return f;
+    }
+    f.entropy = s.S == 0.f ? 0.f : f.ln - kLn2 * (s.T / s.S);
+    const int64_t y = C.labels ? label_of(C, row) : -1;
+    f.logprob = y < 0 ? 0.f : y >= C.V ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (a.x - s.m) - f.ln;
+    return f;
+}
+
+__device__ __forceinline__ void store_results(const ClassCall& C, int64_t row, const Found& f)
+{
+    if (C.logprob) C.logprob[row] = f.logprob;
+    if (C.entropy) C.entropy[row] = f.entropy;
+    if (C.loss) C.loss[row] = f.loss;
+}
+
+__device__ __forceinline__ void store_likeliest(const ClassCall& C, int64_t row, const Sums& s, float ln, uint64_t key, int i)
+{
+    if (i >= C.top_k) return;
+    const int64_t at = row * C.top_k + i;
+    const uint32_t col = key ? 0xFFFFFFFFu - (uint32_t)key : (uint32_t)i;  // (a row of NaN leaves none)
+    const float x = key_value((uint32_t)(key >> 32));
+    C.top_data[at] = key == 0 || s.S != s.S ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (x - s.m) - ln;
+    if (C.top_index_bytes == 1) ((uint8_t*)C.top_index)[at] = (uint8_t)col;
+    else if (C.top_index_bytes == 2) ((uint16_t*)C.top_index)[at] = (uint16_t)col;
+    else ((uint32_t*)C.top_index)[at] = col;
+}
+
+// dx = e (A + B d) + g at the given class
+struct Slope { float A, B, g; int64_t y; };
+__device__ __forceinline__ Slope row_slope(const ClassCall& C, int64_t row, const Sums& s, const Asked& a, const Found& f)
+{
+    const float inverse = 1.f / s.S;
+    if (C.index) {
+        const float g = C.dloss[row] * C.scale;
+        return {s.S == 0.f ? 0.f : g * a.Q * inverse, 0.f, s.S == 0.f ? 0.f : g, -1};
+    }
+    const int64_t y = C.labels ? label_of(C, row) : -1;
+    const float g = !C.dlogprob || y < 0 ? 0.f : y >= C.V ? __builtin_nanf("") : C.dlogprob[row], u = C.dentropy ? C.dentropy[row] : 0.f;
+    if (s.S == 0.f) return {g != g ? g : 0.f, 0.f, 0.f, -1};
+    return {(-g + u * (f.ln - f.entropy)) * inverse, -u * kLn2 * inverse, g, y};
+}
+
+// Columns [first, last) of a row by a workgroup: their sums, and the likeliest of them in every wavefront
+template <int VT, bool TOP>
+__device__ __forceinline__ Sums sum_columns(const ClassCall& C, int64_t row, int first, int last, Likeliest& best)
+{
+    using S = value_store_t<VT>;
+    const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
+    const float c = C.scale * kLog2e;
+    Sums sums = no_sums();
+    bool begun = false;
+    for (int base = first; base < last; base += kThreads * kRowUnit) {
+        const int col = base + threadIdx.x * kRowUnit;
+        float v[kRowUnit];
+        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
+        const float top = largest(v);
+        absorb(sums, v, top, c);
+        if constexpr (TOP) best.offer(v, top, col, last - col, !begun);
+        begun = true;
+    }
+    return sums;
+}
+
+// Their gradient; distillation's entries in these columns follow
+template <int VT, bool DISTILL>
+__device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
+{
+    using S = value_store_t<VT>;
+    const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
+    S* dx = (S*)C.dlogits + row * C.V;
+    const float c = C.scale * kLog2e;
+    const auto slope = [&](float v) {
+        const float d = fmaxf((v - s.m) * c, -kFar);
+        return exp2_of(d) * (DISTILL ? k.A : fmaf(k.B, d, k.A));
+    };
+    for (int base = first; base < last; base += kThreads * kRowUnit) {
+        const int col = base + threadIdx.x * kRowUnit;
+        if (col >= last) break;
+        float v[kRowUnit];
+        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) v[j] = slope(v[j]);
+        if (!DISTILL && (uint64_t)(k.y - col) < kRowUnit) {
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j) v[j] += j == (int)(k.y - col) ? k.g : 0.f;
+        }
+        store_row_unit<VT>(dx + col, last - col, v);
+    }
+    if constexpr (DISTILL) {
+        __syncthreads();  // what is stored above at their columns is stored again
+        for (int i = threadIdx.x; i < C.k; i += kThreads) {
+            const int col = E->col[i];
+            if (col < first || col >= last) continue;
+            float q = 0.f;
+            bool mine = true;  // of several entries of a column the first one has the sum
+            for (int j = 0; j < C.k; ++j)
+                if (E->col[j] == col) {
+                    mine &= j >= i;
+                    q += E->q[j];
+                }
+            if (mine) dx[col] = round_value<VT>(fmaf(-k.g, q, slope(E->x[i])));
+        }
+    }
+}
+
+// A workgroup a row
+template <int VT, bool DISTILL, bool GRAD, bool TOP>
+__global__ void __launch_bounds__(kThreads) class_rows_kernel(ClassCall C)
+{
+    __shared__ Sums sums_room[kWaves];
+    __shared__ float room[kWaves];
+    __shared__ std::conditional_t<DISTILL, Entries, int> entries;
+    __shared__ uint64_t keys[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
+    Likeliest best;
+    if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
+    Asked asked;
+    if constexpr (DISTILL) asked = take_entries<VT>(C, row, entries, room);
+    else asked = given_class<VT>(C, row);
+    Sums s = sum_columns<VT, TOP>(C, row, 0, C.V, best);
+    s = join_workgroup(s, C.scale * kLog2e, sums_room);
+    const Found f = row_results(C, row, s, asked);
+    if constexpr (TOP) {
+        best.end();
+        keys[wave][lane] = best.mine;
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < kWaves; ++w) best.mine = merge_keys(best.mine, keys[w][lane], lane);
+            store_likeliest(C, row, s, f.ln, best.mine, lane);
+        }
+    }
+    if (threadIdx.x == 0) store_results(C, row, f);
+    if constexpr (GRAD) {
+        const Slope k = row_slope(C, row, s, asked, f);
+        if constexpr (DISTILL) store_gradient<VT, true>(C, row, 0, C.V, s, k, &entries);
+        else store_gradient<VT, false>(C, row, 0, C.V, s, k, nullptr);
+    }
+}
+
+// ---- rows in segments ----
+
+struct Parts {
+    int segments, width;  // columns of a segment
+    Sums* sums;           // [N x segments]
+    Asked* asked;         // [N]
+    uint64_t* keys;       // [N x segments x top_k]
+};
+
+template <int VT, bool DISTILL, bool TOP>
+__global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Parts P)
+{
+    __shared__ Sums sums_room[kWaves];
+    __shared__ float room[kWaves];
+    __shared__ std::conditional_t<DISTILL, Entries, int> entries;
+    __shared__ uint64_t keys[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
+    const int64_t row = blockIdx.x / P.segments;
+    const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
+    Likeliest best;
+    if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
+    if (segment == 0) {
+        Asked asked;
+        if constexpr (DISTILL) asked = take_entries<VT>(C, row, entries, room);
+        else asked = given_class<VT>(C, row);
+        if (threadIdx.x == 0) P.asked[row] = asked;
+    }
+    Sums s = sum_columns<VT, TOP>(C, row, first, last, best);
+    s = join_workgroup(s, C.scale * kLog2e, sums_room);
+    if (threadIdx.x == 0) P.sums[blockIdx.x] = s;
+    if constexpr (TOP) {
+        best.end();
+        keys[wave][lane] = best.mine;
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < kWaves; ++w) best.mine = merge_keys(best.mine, keys[w][lane], lane);
+            if (lane < C.top_k) P.keys[(int64_t)blockIdx.x * C.top_k + lane] = best.mine;
+        }
+    }
+}
+
+__device__ __forceinline__ Sums join_segments(const ClassCall& C, const Parts& P, int64_t row, Sums* room)
+{
+    Sums s = no_sums();
+    for (int i = threadIdx.x; i < P.segments; i += kThreads) s = join(s, P.sums[row * P.segments + i], C.scale * kLog2e);
+    return join_workgroup(s, C.scale * kLog2e, room);
+}
+
+template <bool TOP>
+__global__ void __launch_bounds__(kThreads) class_join_kernel(ClassCall C, Parts P)
+{
+    __shared__ Sums sums_room[kWaves];
+    __shared__ uint64_t keys[kWaves][kWave];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
+    const Sums s = join_segments(C, P, row, sums_room);
+    const Found f = row_results(C, row, s, P.asked[row]);
+    if constexpr (TOP) {
+        uint64_t mine = 0;
+        for (int i = wave; i < P.segments; i += kWaves)
+            mine = merge_keys(mine, lane < C.top_k ? P.keys[(row * P.segments + i) * C.top_k + lane] : 0, lane);
+        keys[wave][lane] = mine;
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < kWaves; ++w) mine = merge_keys(mine, keys[w][lane], lane);
+            store_likeliest(C, row, s, f.ln, mine, lane);
+        }
+    }
+    if (threadIdx.x == 0) store_results(C, row, f);
+}
+
+template <int VT, bool DISTILL>
+__global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, Parts P)
+{
+    __shared__ Sums sums_room[kWaves];
+    __shared__ float room[kWaves];
+    __shared__ std::conditional_t<DISTILL, Entries, int> entries;
+    const int64_t row = blockIdx.x / P.segments;
+    const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
+    const Sums s = join_segments(C, P, row, sums_room);
+    const Asked asked = P.asked[row];
+    if constexpr (DISTILL) take_entries<VT>(C, row, entries, room);  // (x of other segments may have been overwritten: only those of this one are used)
+    const Found f = row_results(C, row, s, asked);
+    if (segment == 0 && threadIdx.x == 0) store_results(C, row, f);
+    const Slope k = row_slope(C, row, s, asked, f);
+    if constexpr (DISTILL) store_gradient<VT, true>(C, row, first, last, s, k, &entries);
+    else store_gradient<VT, false>(C, row, first, last, s, k, nullptr);
+}
+
+// Segments of a row
+struct Cut { int segments, width; };
+constexpr int kLeastSegment = kThreads * kRowUnit;
+Cut cut_of(int64_t N, int V)
+{
+    constexpr int kGroups = 512;
+    if (N >= kGroups || V < 2 * kLeastSegment) return {1, V};
+    const int most = (V + kLeastSegment - 1) / kLeastSegment, wanted = (int)((kGroups + N - 1) / std::max<int64_t>(N, 1));
+    const int per = (most + std::min(most, wanted) - 1) / std::min(most, wanted);
+    return {(most + per - 1) / per, per * kLeastSegment};
+}
+
+int64_t up16(int64_t n) { return (n + 15) & ~15ll; }
+
+template <int VT, bool DISTILL, bool GRAD, bool TOP>
+maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
+{
+    const Cut cut = cut_of(C.N, C.V);
+    if (cut.segments == 1) {
+        if (C.N > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
+        hipLaunchKernelGGL((class_rows_kernel<VT, DISTILL, GRAD, TOP>), dim3((unsigned)C.N), dim3(kThreads), 0, s, C);
+        MAXK_LAUNCH_CHECK();
+        return MAXK_OK;
+    }
+    char* at = (char*)workspace;
+    Parts P = {cut.segments, cut.width, (Sums*)at, nullptr, nullptr};
+    at += up16(C.N * cut.segments * (int64_t)sizeof(Sums));
+    P.asked = (Asked*)at;
+    at += up16(C.N * (int64_t)sizeof(Asked));
+    P.keys = (uint64_t*)at;
+    const unsigned groups = (unsigned)(C.N * cut.segments);
+    hipLaunchKernelGGL((class_parts_kernel<VT, DISTILL, TOP>), dim3(groups), dim3(kThreads), 0, s, C, P);
+    MAXK_LAUNCH_CHECK();
+    if constexpr (GRAD) hipLaunchKernelGGL((class_gradient_kernel<VT, DISTILL>), dim3(groups), dim3(kThreads), 0, s, C, P);
+    else hipLaunchKernelGGL((class_join_kernel<TOP>), dim3((unsigned)C.N), dim3(kThreads), 0, s, C, P);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
+template <int VT>
+maxk_status run_type(const ClassCall& C, void* workspace, hipStream_t s)
+{
+    if (C.index) return C.dlogits ? run_classes<VT, true, true, false>(C, workspace, s) : run_classes<VT, true, false, false>(C, workspace, s);
+    if (C.dlogits) return run_classes<VT, false, true, false>(C, workspace, s);
+    return C.top_data ? run_classes<VT, false, false, true>(C, workspace, s) : run_classes<VT, false, false, false>(C, workspace, s);
+}
+
+}  // namespace
+
+int64_t classes_workspace(int64_t N, int32_t V, int32_t top_k)
+{
+    const Cut cut = cut_of(N, V);
+    if (cut.segments == 1) return 0;
+    return up16(N * cut.segments * (int64_t)sizeof(Sums)) + up16(N * (int64_t)sizeof(Asked)) + N * cut.segments * (int64_t)top_k * 8;
+}
+
+maxk_status launch_classes(const ClassCall& C, int value_type, void* workspace, hipStream_t s)
+{
+    if (value_type == MAXK_VALUE_F32) return run_type<MAXK_VALUE_F32>(C, workspace, s);
+    if (value_type == MAXK_VALUE_BF16) return run_type<MAXK_VALUE_BF16>(C, workspace, s);
+    return run_type<MAXK_VALUE_F16>(C, workspace, s);
+}
+
+}  // namespace maxk

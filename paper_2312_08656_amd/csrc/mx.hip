@@ -89,6 +89,18 @@ MAXK_API maxk_status maxk_mx_linear(const uint8_t* d_x_codes, const uint8_t* d_x
                             (hipStream_t)stream);
 }
 
+MAXK_API maxk_status maxk_mx_matvec(const void* d_X, int32_t value_type, int64_t N, const uint8_t* d_w_codes, const uint8_t* d_w_scales, int32_t din,
+                                    int32_t dout, const float* d_bias, void* d_Y, int32_t y_value_type, void* stream)
+{
+    if (bad_type(value_type) || bad_type(y_value_type)) return MAXK_INVALID_ARGUMENT;
+    if (N < 0 || din < 1 || dout < 1) return MAXK_INVALID_ARGUMENT;
+    if (din > MAXK_MX_MAX_DIM || dout > MAXK_MAX_CLASSES || N > MAXK_MX_MATVEC_MAX_ROWS) return MAXK_UNSUPPORTED;
+    if (N == 0) return MAXK_OK;
+    if (!d_X || !aligned(d_X, bytes_of(value_type)) || bad_codes(d_w_codes, d_w_scales) || !d_Y || !aligned(d_Y, bytes_of(y_value_type)) || !aligned(d_bias, 4))
+        return MAXK_INVALID_ARGUMENT;
+    return launch_mx_matvec(d_X, value_type, N, {d_w_codes, d_w_scales, MAXK_MX_4}, din, dout, d_bias, d_Y, y_value_type, (hipStream_t)stream);
+}
+
 MAXK_API int64_t maxk_mx_weight_grad_workspace(int64_t N, int32_t din, int32_t dout)
 {
     if (const maxk_status st = bad_sizes(N, din, dout)) return st;

@@ -53,13 +53,6 @@ __device__ __forceinline__ void load_unit(const value_store_t<VT>* X, const Unit
     }
 }
 
-// the largest of four neighbouring lanes
-__device__ __forceinline__ uint32_t max_of_four(uint32_t x)
-{
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));   // quad_perm [1,0,3,2]
-    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));  // quad_perm [2,3,0,1]
-}
-
 template <int VT, Rows R, int FMT>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const value_store_t<VT>* __restrict__ X, int64_t units, int din, int nb,
                                                             uint8_t* __restrict__ codes, uint8_t* __restrict__ scales)
@@ -74,37 +67,8 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const value_store_t<
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         const int64_t u = base + i * kThreads;
-        if (u >= units) break;  // whole blocks of four lanes: units are a multiple of 4
-        uint32_t top = 0;       // patterns of magnitudes are in the magnitudes' order, Inf and NaN above all others
-#pragma unroll
-        for (int j = 0; j < kUnit; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7FFFFFFFu);
-        uint32_t s = max_of_four(top) >> 23;
-        const bool finite = s != 255u;
-        if constexpr (FMT == MAXK_MX_8) {
-            uint32_t w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t q[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // adding 1.5 * 2^23 rounds to a whole number, halfway cases to even, and leaves it in the low byte
-                    const float y = __builtin_amdgcn_ldexpf(x[i][4 * h + j], 133 - (int)s);
-                    q[j] = __float_as_uint(__builtin_amdgcn_fmed3f(y, -127.f, 127.f) + 0x1.8p23f);
-                }
-                const uint32_t low = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), high = __builtin_amdgcn_perm(q[3], q[2], 0x04000C0Cu);
-                w[h] = finite ? low | high : 0u;
-            }
-            *reinterpret_cast<uint2*>(codes + u * kUnit) = make_uint2(w[0], w[1]);
-        } else {
-            if (finite) s = s > 2u ? s - 2u : 0u;
-            const float scale = mx_scale(s);
-            uint32_t w = 0;  // the conversion divides by the scale, rounds to nearest even and saturates
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][0], x[i][1], scale, 0);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][2], x[i][3], scale, 1);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][4], x[i][5], scale, 2);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[i][6], x[i][7], scale, 3);
-            *reinterpret_cast<uint32_t*>(codes + u * (kUnit / 2)) = finite ? w : 0u;
-        }
+        if (u >= units) break;
+        const uint32_t s = encode_unit<FMT>(x[i], codes + u * (FMT == MAXK_MX_8 ? kUnit : kUnit / 2));  // whole blocks of four lanes: units are a multiple of 4
         if ((threadIdx.x & 3) == 0) scales[u >> 2] = (uint8_t)s;
     }
 }

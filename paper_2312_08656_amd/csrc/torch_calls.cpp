@@ -29,11 +29,21 @@ decltype(&maxk_mx_weight_grad_cbsr) weight_grad_cbsr_call;
 decltype(&maxk_mx_input_grad) input_grad_call;
 decltype(&maxk_mx_input_grad_cbsr) input_grad_cbsr_call;
 
+decltype(&maxk_mx_matvec) matvec_call;
+decltype(&maxk_rms_norm) rms_norm_call;
+decltype(&maxk_rms_norm_grad_workspace) rms_norm_grad_workspace_call;
+decltype(&maxk_rms_norm_grad) rms_norm_grad_call;
+decltype(&maxk_classes_workspace) classes_workspace_call;
+decltype(&maxk_logprobs) logprobs_call;
+decltype(&maxk_logprobs_grad) logprobs_grad_call;
+decltype(&maxk_distill) distill_call;
+decltype(&maxk_distill_grad) distill_grad_call;
+
 PyObject* check;  // (status, name of the call): raises; held for good
 
 void bind(const std::vector<uintptr_t>& at, const py::function& raise)
 {
-    TORCH_CHECK(at.size() == 13, "thirteen addresses");
+    TORCH_CHECK(at.size() == 22, "twenty-two addresses");
     topk_call = reinterpret_cast<decltype(topk_call)>(at[0]);
     forward_call = reinterpret_cast<decltype(forward_call)>(at[1]);
     forward_noalloc_call = reinterpret_cast<decltype(forward_noalloc_call)>(at[2]);
@@ -47,6 +57,15 @@ void bind(const std::vector<uintptr_t>& at, const py::function& raise)
     weight_grad_cbsr_call = reinterpret_cast<decltype(weight_grad_cbsr_call)>(at[10]);
     input_grad_call = reinterpret_cast<decltype(input_grad_call)>(at[11]);
     input_grad_cbsr_call = reinterpret_cast<decltype(input_grad_cbsr_call)>(at[12]);
+    matvec_call = reinterpret_cast<decltype(matvec_call)>(at[13]);
+    rms_norm_call = reinterpret_cast<decltype(rms_norm_call)>(at[14]);
+    rms_norm_grad_workspace_call = reinterpret_cast<decltype(rms_norm_grad_workspace_call)>(at[15]);
+    rms_norm_grad_call = reinterpret_cast<decltype(rms_norm_grad_call)>(at[16]);
+    classes_workspace_call = reinterpret_cast<decltype(classes_workspace_call)>(at[17]);
+    logprobs_call = reinterpret_cast<decltype(logprobs_call)>(at[18]);
+    logprobs_grad_call = reinterpret_cast<decltype(logprobs_grad_call)>(at[19]);
+    distill_call = reinterpret_cast<decltype(distill_call)>(at[20]);
+    distill_grad_call = reinterpret_cast<decltype(distill_grad_call)>(at[21]);
     Py_XDECREF(std::exchange(check, py::function(raise).release().ptr()));
 }
 
@@ -360,6 +379,202 @@ bool mx_input_grad(const py::handle& values_, const py::handle& index_, const py
     });
 }
 
+// ---- both ends of a classifier ----
+
+// Whether tensors (null: none) are the current device's, whose stream a call takes
+template <typename... T>
+bool here(const T*... tensors)
+{
+    const c10::DeviceIndex device = c10::hip::current_device();
+    return ((!tensors || tensors->device().index() == device) && ...);
+}
+
+const void* address(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+void* place(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+float* floats(const at::Tensor* t) { return t ? static_cast<float*>(t->data_ptr()) : nullptr; }
+
+// Arguments that may be None; `good` turns false where one is something else than the call takes
+struct Optionals {
+    bool good = true;
+    const at::Tensor* like(const py::handle& x, const at::Tensor& X)  // a matrix of X's shape and type
+    {
+        if (x.is_none()) return nullptr;
+        const at::Tensor* t = matrix(x, X.size(0), X.size(1));
+        good &= t && t->scalar_type() == X.scalar_type();
+        return t;
+    }
+    const at::Tensor* floats(const py::handle& x, int64_t n)
+    {
+        if (x.is_none()) return nullptr;
+        const at::Tensor* t = vector(x, n);
+        good &= t != nullptr;
+        return t;
+    }
+    const at::Tensor* labels(const py::handle& x, int64_t n)
+    {
+        if (x.is_none()) return nullptr;
+        const at::Tensor* t = plain(x);
+        if (t && (t->dim() != 1 || !t->is_contiguous() || t->size(0) != n || (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong))) t = nullptr;
+        good &= t != nullptr;
+        return t;
+    }
+};
+
+int label_bytes(const at::Tensor* t) { return !t ? 0 : t->scalar_type() == at::kLong ? 8 : 4; }
+
+// The workspace of a call that needs `need` bytes: the one that is given, or `own`, made here
+bool workspace_for(const py::handle& given, int64_t need, const at::Tensor& X, at::Tensor& own, const at::Tensor*& workspace)
+{
+    workspace = nullptr;
+    if (need < 0) return false;
+    if (!given.is_none()) {
+        workspace = plain(given);
+        return workspace && workspace->is_contiguous() && workspace->scalar_type() == at::kByte && here(workspace);
+    }
+    if (need == 0) return true;
+    try {
+        own = at::empty({need}, X.options().dtype(at::kByte));
+    } catch (const c10::Error&) {  // no memory: said by the call from Python
+        return false;
+    }
+    workspace = &own;
+    return true;
+}
+int64_t room(const at::Tensor* workspace) { return workspace ? workspace->numel() : 0; }
+
+const at::Tensor* rows(const py::handle& x, int64_t most)  // a matrix of values of a width that the call takes
+{
+    const at::Tensor* t = matrix(x, -1, -1);
+    return t && value_type(*t) >= 0 && t->size(1) <= most ? t : nullptr;
+}
+
+bool mx_matvec(const py::handle& X_, const py::handle& wc, const py::handle& ws, const py::handle& Y_, const py::handle& bias_)
+{
+    const at::Tensor *X = rows(X_, MAXK_MX_MAX_DIM), *Y = rows(Y_, MAXK_MAX_CLASSES);
+    if (!X || !Y || Y->size(0) != X->size(0)) return false;
+    const Stored W = stored(wc, ws, Y->size(1), X->size(1), true);
+    Optionals given;
+    const at::Tensor* bias = given.floats(bias_, Y->size(1));
+    if (!W || !given.good || !here(X, Y, W.codes, W.scales, bias)) return false;
+    return made("maxk_mx_matvec", [&, s = stream()](const char*) {
+        return matvec_call(X->data_ptr(), value_type(*X), X->size(0), W.code(), W.scale(), (int32_t)X->size(1), (int32_t)Y->size(1), floats(bias), Y->data_ptr(),
+                           value_type(*Y), s);
+    });
+}
+
+bool rms_norm(const py::handle& X_, const py::handle& gamma_, const py::handle& Y_, const py::handle& codes_, const py::handle& scales_,
+              const py::handle& residual_, const py::handle& H_, const py::handle& rstd_, double eps)
+{
+    const at::Tensor* X = rows(X_, MAXK_NORM_MAX_DIM);
+    if (!X) return false;
+    const int64_t N = X->size(0), dim = X->size(1);
+    Optionals given;
+    const at::Tensor *gamma = vector(gamma_, dim), *Y = given.like(Y_, *X), *residual = given.like(residual_, *X), *H = given.like(H_, *X),
+                     *rstd = given.floats(rstd_, N);
+    Stored to = {};
+    if (!codes_.is_none()) {
+        to = stored(codes_, scales_, N, dim, false);
+        given.good &= (bool)to;
+    } else {
+        given.good &= scales_.is_none();
+    }
+    if (!given.good || !gamma || !residual != !H || (!Y && !to) || !here(X, gamma, Y, to.codes, to.scales, residual, H, rstd)) return false;
+    return made("maxk_rms_norm", [&, s = stream()](const char*) {
+        return rms_norm_call(X->data_ptr(), address(residual), value_type(*X), N, (int32_t)dim, floats(gamma), eps, place(H), place(Y), to ? to.format : 0,
+                             place(to.codes), static_cast<uint8_t*>(place(to.scales)), floats(rstd), s);
+    });
+}
+
+bool rms_norm_grad(const py::handle& dY_, const py::handle& H_, const py::handle& gamma_, const py::handle& rstd_, const py::handle& dX_,
+                   const py::handle& dgamma_, const py::handle& dH_, const py::handle& workspace_)
+{
+    const at::Tensor* H = rows(H_, MAXK_NORM_MAX_DIM);
+    if (!H) return false;
+    const int64_t N = H->size(0), dim = H->size(1);
+    Optionals given;
+    const at::Tensor *dY = given.like(dY_, *H), *dX = given.like(dX_, *H), *dH = given.like(dH_, *H), *dgamma = given.floats(dgamma_, dim),
+                     *gamma = vector(gamma_, dim), *rstd = vector(rstd_, N), *workspace;
+    if (!given.good || !dY || !dX || !gamma || !rstd || !here(H, dY, dX, dH, dgamma, gamma, rstd)) return false;
+    at::Tensor own;
+    if (!workspace_for(workspace_, dgamma ? rms_norm_grad_workspace_call(N, (int32_t)dim) : 0, *H, own, workspace)) return false;
+    return made("maxk_rms_norm_grad", [&, s = stream()](const char*) {
+        return rms_norm_grad_call(dY->data_ptr(), H->data_ptr(), address(dH), value_type(*H), N, (int32_t)dim, floats(gamma), floats(rstd), dX->data_ptr(),
+                                  floats(dgamma), place(workspace), room(workspace), s);
+    });
+}
+
+bool logprobs(const py::handle& logits_, const py::handle& labels_, const py::handle& logprob_, const py::handle& entropy_, const py::handle& data_,
+              const py::handle& index_, const py::handle& workspace_)
+{
+    const at::Tensor* logits = rows(logits_, MAXK_MAX_CLASSES);
+    if (!logits) return false;
+    const int64_t N = logits->size(0), V = logits->size(1);
+    Optionals given;
+    const at::Tensor *labels = given.labels(labels_, N), *logprob = given.floats(logprob_, N), *entropy = given.floats(entropy_, N), *data = nullptr,
+                     *index = nullptr, *workspace;
+    int64_t k = 0;
+    if (!data_.is_none()) {
+        data = matrix(data_, N, -1);
+        if (!data || data->scalar_type() != at::kFloat) return false;
+        k = data->size(1);
+        index = matrix(index_, N, k);
+        if (!index || !index_bytes(*index) || k < 1 || k > MAXK_MAX_ALTERNATIVES) return false;
+    } else if (!index_.is_none()) {
+        return false;
+    }
+    if (!given.good || (logprob && !labels) || (!logprob && !entropy && !data) || !here(logits, labels, logprob, entropy, data, index)) return false;
+    at::Tensor own;
+    if (!workspace_for(workspace_, classes_workspace_call(N, (int32_t)V, (int32_t)k), *logits, own, workspace)) return false;
+    return made("maxk_logprobs", [&, s = stream()](const char*) {
+        return logprobs_call(logits->data_ptr(), value_type(*logits), N, (int32_t)V, address(labels), label_bytes(labels), floats(logprob), floats(entropy),
+                             floats(data), place(index), index ? index_bytes(*index) : 0, (int32_t)k, place(workspace), room(workspace), s);
+    });
+}
+
+bool logprobs_grad(const py::handle& logits_, const py::handle& dlogits_, const py::handle& labels_, const py::handle& dlogprob_, const py::handle& dentropy_,
+                   const py::handle& logprob_, const py::handle& entropy_, const py::handle& workspace_)
+{
+    const at::Tensor* logits = rows(logits_, MAXK_MAX_CLASSES);
+    if (!logits) return false;
+    const int64_t N = logits->size(0), V = logits->size(1);
+    Optionals given;
+    const at::Tensor *labels = given.labels(labels_, N), *dlogprob = given.floats(dlogprob_, N), *dentropy = given.floats(dentropy_, N),
+                     *logprob = given.floats(logprob_, N), *entropy = given.floats(entropy_, N), *dlogits = given.like(dlogits_, *logits), *workspace;
+    if (!given.good || !dlogits || (!dlogprob && !dentropy) || ((dlogprob || logprob) && !labels) ||
+        !here(logits, dlogits, labels, dlogprob, dentropy, logprob, entropy))
+        return false;
+    at::Tensor own;
+    if (!workspace_for(workspace_, classes_workspace_call(N, (int32_t)V, 0), *logits, own, workspace)) return false;
+    return made("maxk_logprobs_grad", [&, s = stream()](const char*) {
+        return logprobs_grad_call(logits->data_ptr(), value_type(*logits), N, (int32_t)V, address(labels), label_bytes(labels), floats(dlogprob), floats(dentropy),
+                                  floats(logprob), floats(entropy), dlogits->data_ptr(), place(workspace), room(workspace), s);
+    });
+}
+
+// the loss, or (dlogits_ not None) its gradient
+bool distill(const py::handle& logits_, const py::handle& data_, const py::handle& index_, const py::handle& dloss_, const py::handle& dlogits_,
+             double temperature, const py::handle& loss_, const py::handle& workspace_)
+{
+    const at::Tensor *logits = rows(logits_, MAXK_MAX_CLASSES), *data = rows(data_, MAXK_DISTILL_MAX_K);
+    if (!logits || !data || data->size(0) != logits->size(0)) return false;
+    const int64_t N = logits->size(0), V = logits->size(1), k = data->size(1);
+    const at::Tensor* index = matrix(index_, N, k);
+    if (!index || !index_bytes(*index)) return false;
+    Optionals given;
+    const at::Tensor *dloss = given.floats(dloss_, N), *loss = given.floats(loss_, N), *dlogits = given.like(dlogits_, *logits), *workspace;
+    if (!given.good || (dlogits ? !dloss : !loss) || !here(logits, data, index, dloss, loss, dlogits)) return false;
+    at::Tensor own;
+    if (!workspace_for(workspace_, classes_workspace_call(N, (int32_t)V, 0), *logits, own, workspace)) return false;
+    return made(dlogits ? "maxk_distill_grad" : "maxk_distill", [&, s = stream()](const char*) {
+        const int32_t v = (int32_t)V, n = (int32_t)k;
+        if (dlogits)
+            return distill_grad_call(logits->data_ptr(), value_type(*logits), N, v, data->data_ptr(), value_type(*data), index->data_ptr(), index_bytes(*index), n,
+                                     temperature, floats(dloss), floats(loss), dlogits->data_ptr(), place(workspace), room(workspace), s);
+        return distill_call(logits->data_ptr(), value_type(*logits), N, v, data->data_ptr(), value_type(*data), index->data_ptr(), index_bytes(*index), n,
+                            temperature, floats(loss), place(workspace), room(workspace), s);
+    });
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_torch_calls, m)
@@ -377,4 +592,10 @@ PYBIND11_MODULE(_torch_calls, m)
     m.def("mx_linear", &mx_linear);
     m.def("mx_weight_grad", &mx_weight_grad);
     m.def("mx_input_grad", &mx_input_grad);
+    m.def("mx_matvec", &mx_matvec);
+    m.def("rms_norm", &rms_norm);
+    m.def("rms_norm_grad", &rms_norm_grad);
+    m.def("logprobs", &logprobs);
+    m.def("logprobs_grad", &logprobs_grad);
+    m.def("distill", &distill);
 }

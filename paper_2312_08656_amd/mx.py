@@ -15,6 +15,7 @@ from .binding import MaxKError
 
 MX_8, MX_4 = 0, 1
 _MAX_DIM = 65536  # MAXK_MX_MAX_DIM
+_MAX_CLASSES = 1 << 24  # MAXK_MAX_CLASSES
 _UNSUPPORTED = -2
 _FORMAT = {torch.int8: MX_8, torch.uint8: MX_4}
 
@@ -107,6 +108,27 @@ def maxk_mx_linear(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch
         _b._dev(x_codes, torch.uint8, "x_codes"), _b._dev(x_scales, torch.uint8, "x_scales"), N, _b._dev(w_codes, torch.uint8, "w_codes"),
         _b._dev(w_scales, torch.uint8, "w_scales"), din, dout, None if bias is None else _b._dev(bias, torch.float32, "bias"),
         _b._dev(Y, Y.dtype, "Y"), _value(Y, "maxk_mx_linear: Y"), _b._stream()), "maxk_mx_linear")
+
+
+def maxk_mx_matvec(X: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, Y: torch.Tensor, bias: Optional[torch.Tensor] = None) -> None:
+    """Y [N, dout] is overwritten with X W^T + bias for few rows X [N, din] that are not rounded, W [dout, din] in 4 bits; X and Y each float32, bfloat16
+    or float16.  16 rows cost about what one does."""
+    what = "maxk_mx_matvec"
+    if _b._FAST is not None and _b._FAST.mx_matvec(X, w_codes, w_scales, Y, bias):
+        return
+    N, din = _matrix(X, f"{what}: X")
+    if Y.dim() != 2 or Y.shape[0] != N:
+        raise MaxKError(f"{what}: Y must be [N, dout]")
+    dout = Y.shape[1]
+    if dout > _MAX_CLASSES:
+        _b._check(_UNSUPPORTED, what)
+    _stored(w_codes, w_scales, dout, din, f"{what}: W", True)
+    if bias is not None and tuple(bias.shape) != (dout,):
+        raise MaxKError(f"{what}: bias must be [dout]")
+    args = (_b._dev(X, X.dtype, "X"), _value(X, f"{what}: X"), N, _b._dev(w_codes, torch.uint8, "w_codes"), _b._dev(w_scales, torch.uint8, "w_scales"), din, dout,
+            None if bias is None else _b._dev(bias, torch.float32, "bias"), _b._dev(Y, Y.dtype, "Y"), _value(Y, f"{what}: Y"))
+    _b._here(what, X, w_codes, w_scales, Y, bias)
+    _b._check(_b.load_library().maxk_mx_matvec(*args, _b._stream()), what)
 
 
 def _weight_grad_shapes(codes, scales, N, dout, dW, db, what):

@@ -1,0 +1,204 @@
+"""Log probabilities, entropies, the likeliest classes and the logits' gradient against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import heads_common as hc
+import paper_2312_08656_amd as maxk
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+def inputs(N, V, dtype, seed, masked=True):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = 3 * torch.randn(N, V, generator=gen, device="cuda")
+    labels = torch.randint(V, (N,), generator=gen, device="cuda")
+    x.scatter_add_(1, labels.unsqueeze(1), 5 * torch.randn(N, 1, generator=gen, device="cuda"))
+    if masked and V > 4:
+        x[:, V - 1 - V // 50:] = -INF
+    if N > 6:
+        labels[3] = -1
+        labels[4] = -100
+        x[5] = x[5, 0].clone()  # all the same
+        if masked:
+            x[6] = -INF  # nothing is left
+    return x.to(dtype), labels, gen
+
+
+def results(N, k=0, ib=torch.int32):
+    return (torch.full((N,), 7.0, device="cuda"), torch.full((N,), 7.0, device="cuda"),
+            torch.full((N, k), 7.0, device="cuda") if k else None, torch.full((N, k), 7, device="cuda").to(ib) if k else None)
+
+
+def check(x, labels, k=0, ib=torch.int32):
+    N, V = x.shape
+    logprob, entropy, data, index = results(N, k, ib)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    lp, lp_bound, H, H_bound, R = hc.logprobs(x, labels)
+    hc.close(logprob, lp, lp_bound)
+    hc.close(entropy, H, H_bound)
+    if k:
+        want = hc.likeliest(x, k)
+        assert np.array_equal(index.cpu().numpy().astype(np.int64), want)
+        top = np.take_along_axis(R.logp, want, 1)
+        d = np.abs(np.where(np.isfinite(top), top, 0))
+        hc.close(data, top, R.u + 4 * hc.U * (d + 2 * np.abs(R.lnS)))
+    return logprob, entropy, R
+
+
+# widths around a lane's, a team's, a wavefront's and a workgroup's columns and rounds
+WIDTHS = [1, 2, 5, 8, 9, 31, 32, 41, 47, 64, 65, 100, 128, 200, 256, 257, 500, 512, 513, 1000, 1024, 1025, 2000, 2048, 2049, 4095, 4097, 10007]
+
+
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("V", WIDTHS)
+def test_logprobs(V, dtype):
+    N = 37
+    x, labels, _ = inputs(N, V, dtype, V)
+    check(x, labels, min(V, 5))
+    check(x, labels.to(torch.int32))
+
+
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("N,V", [(1, 32768), (3, 131072), (2, 50021), (700, 4099), (1, 1), (5, 9000), (64, 20011), (3001, 47), (1500, 300)])
+def test_few_and_many_rows(N, V, dtype):
+    x, labels, _ = inputs(N, V, dtype, N + V)
+    check(x, labels, min(V, 20))
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 7, 16, 33, 50, 63, 64])
+@pytest.mark.parametrize("V", [64, 65, 100, 256, 700, 1500, 5000, 40000])
+def test_alternatives(k, V):
+    for dtype in (torch.float32, torch.bfloat16):  # (many equal values in 16 bits)
+        x, labels, _ = inputs(9, V, dtype, k + V)
+        check(x, labels, k, torch.uint8 if V <= 256 else torch.uint16 if k % 2 else torch.int32)
+
+
+@pytest.mark.parametrize("V", [40, 130, 600, 1500, 3000, 30000])
+def test_alternatives_in_any_order(V):
+    """Rows that rise, fall, are all the same, have the largest last or hold few different values."""
+    up = torch.arange(V, device="cuda", dtype=torch.float32) / V
+    rows = torch.stack([up, up.flip(0), torch.zeros_like(up), torch.where(up > 0.999, 5.0, 0.0), torch.where(up < 1e-3, 5.0, -1.0), (up * 4).floor(),
+                        torch.where(torch.arange(V, device="cuda") % 2 == 0, 0.0, -0.0), torch.full_like(up, -3.4e38), -(up * 8).floor()])
+    labels = torch.arange(rows.shape[0], device="cuda")
+    for k in (1, 20, 40):
+        check(rows, labels, k)
+
+
+def test_masks_of_the_lowest_value_and_of_everything():
+    lowest = torch.finfo(torch.float32).min
+    x = torch.full((4, 100), lowest, device="cuda")
+    x[1, 7] = 2.0
+    x[2] = -INF
+    x[2, 50] = lowest
+    x[3] = -INF
+    labels = torch.tensor([3, 7, 50, 0], device="cuda")
+    logprob, entropy, data, index = results(4, 3)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    ln = np.log(100)
+    assert abs(logprob[0].item() + ln) < 1e-6 and abs(entropy[0].item() - ln) < 1e-6 and index[0].tolist() == [0, 1, 2]
+    assert logprob[1] == 0 and entropy[1] == 0 and index[1].tolist() == [7, 0, 1] and data[1, 0] == 0
+    assert logprob[2] == 0 and entropy[2] == 0 and index[2].tolist() == [50, 0, 1] and data[2, 1] == -INF
+    assert logprob[3] == -INF and entropy[3] == 0 and index[3].tolist() == [0, 1, 2] and (data[3] == -INF).all()
+    dx = torch.full_like(x, 7)
+    maxk.maxk_logprobs_grad(x, dx, labels, torch.ones(4, device="cuda"), torch.ones(4, device="cuda"))
+    assert torch.isfinite(dx).all() and (dx[2:] == 0).all() and abs(dx[0, 3].item() - 0.99) < 1e-6 and dx[1].abs().max() == 0
+
+
+@pytest.mark.parametrize("V", [47, 300, 1500, 9000])
+def test_non_finite(V):
+    x = torch.zeros(4, V, device="cuda")
+    x[0, V // 2] = NAN
+    x[1, V - 1] = INF
+    x[2, 3] = -NAN
+    labels = torch.tensor([0, 1, 2, V], device="cuda")
+    logprob, entropy, data, index = results(4, 5)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    assert torch.isnan(logprob).all() and torch.isnan(entropy[:3]).all() and torch.isnan(data[:3]).all()
+    assert ((index >= 0) & (index < V)).all() and torch.isfinite(entropy[3]) and index[3].tolist() == [0, 1, 2, 3, 4]
+    dx = torch.zeros_like(x)
+    maxk.maxk_logprobs_grad(x, dx, labels, torch.ones(4, device="cuda"))
+    assert torch.isnan(dx).all()
+
+
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("N,V", [(37, V) for V in WIDTHS] + [(1, 32768), (3, 70001), (700, 4099), (2, 131072), (3001, 47)])
+def test_gradient(N, V, dtype):
+    x, labels, gen = inputs(N, V, dtype, 3 * V + N)
+    g, u = (torch.randn(N, generator=gen, device="cuda") for _ in range(2))
+    lp, lp_bound, H, H_bound, R = hc.logprobs(x, labels)
+    for dlogprob, dentropy in ((g, u), (g, None), (None, u)):
+        dx = torch.full_like(x, 7)
+        logprob, entropy, _, _ = results(N)
+        maxk.maxk_logprobs_grad(x, dx, labels, dlogprob, dentropy, logprob=logprob, entropy=entropy)
+        hc.close(logprob, lp, lp_bound)
+        hc.close(entropy, H, H_bound)
+        want, bound = hc.logprobs_grad(R, labels, dlogprob, dentropy)
+        hc.close(dx, want, bound, dtype)
+    own = x.clone()
+    maxk.maxk_logprobs_grad(own, own, labels, None, u)  # in the logits' own memory
+    assert torch.equal(own, dx)
+    maxk.maxk_logprobs_grad(x, own, None, None, u)
+    assert torch.equal(own, dx)
+
+
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+def test_offsets(dtype):
+    """Logits and gradients that start at any element; nothing is written around them."""
+    for N, V in ((9, 47), (5, 301), (7, 3001), (2, 9001)):
+        x, labels, gen = inputs(N, V, dtype, V, masked=False)
+        g = torch.randn(N, generator=gen, device="cuda")
+        want = torch.empty_like(x)
+        maxk.maxk_logprobs_grad(x, want, labels, g)
+        for at, to in ((1, 2), (3, 0), (0, 1), (5, 5)):
+            flat, out = (torch.full((N * V + 16,), 3.0, dtype=dtype, device="cuda") for _ in range(2))
+            flat[at:at + N * V].copy_(x.view(-1))
+            dx = out[to:to + N * V].view(N, V)
+            maxk.maxk_logprobs_grad(flat[at:at + N * V].view(N, V), dx, labels, g)
+            assert torch.equal(dx, want) and (out[:to] == 3).all() and (out[to + N * V:] == 3).all()
+
+
+def test_gradients_are_differences():
+    N, V = 5, 30
+    x, labels, gen = inputs(N, V, torch.float32, 8, masked=False)
+    g, u = (torch.randn(N, generator=gen, device="cuda") for _ in range(2))
+    dx = torch.empty_like(x)
+    maxk.maxk_logprobs_grad(x, dx, labels, g, u)
+    y, has = labels.clamp_min(0).cpu().numpy(), (labels >= 0).cpu().numpy()
+
+    def value(x):
+        lp = x - x.max(1, keepdims=True)
+        lp = lp - np.log(np.exp(lp).sum(1, keepdims=True))
+        return (hc.f64(g) * np.where(has, lp[np.arange(N), y], 0)).sum() - (hc.f64(u)[:, None] * np.exp(lp) * lp).sum()
+
+    base, step = hc.f64(x), 1e-5
+    for n, i in ((0, 0), (0, y[0]), (3, 2), (4, 29), (2, y[2])):
+        up, down = base.copy(), base.copy()
+        up[n, i] += step
+        down[n, i] -= step
+        assert abs((value(up) - value(down)) / (2 * step) - dx[n, i].item()) < 1e-5
+
+
+def test_rows_past_32_bits():
+    """Offsets of more than 2^31 elements, and bytes past 2^32."""
+    N, V = 2300, 1_000_003
+    x = torch.zeros(N, V, dtype=torch.bfloat16, device="cuda")
+    labels = torch.arange(N, device="cuda") * 401
+    x[torch.arange(N, device="cuda"), labels] = 14.0
+    logprob, entropy, data, index = results(N, 2)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    S = np.exp(14.0) + V - 1
+    assert (logprob - (14 - np.log(S))).abs().max() < 1e-4 and torch.equal(index[:, 0].long(), labels)
+    assert torch.equal(index[:, 1].long(), (labels == 0).long())
+    maxk.maxk_logprobs_grad(x, x, labels, torch.full((N,), 1.0, device="cuda"))
+    p = np.exp(14.0) / S
+    rows = torch.arange(N, device="cuda")
+    assert ((x[rows, labels].float() - (1 - p)).abs() <= 2.0 ** -8 * (1 - p) + 1e-5).all()
+    assert ((x[:, -1].float() + 1 / S).abs() <= 2.0 ** -8 / S + 1e-9).all()
+
+
+def test_no_rows():
+    x = torch.empty(0, 9, device="cuda")
+    maxk.maxk_logprobs(x, None, None, torch.empty(0, device="cuda"))
+    maxk.maxk_logprobs_grad(x, x.clone(), None, None, torch.empty(0, device="cuda"))
