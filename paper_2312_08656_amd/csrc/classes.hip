@@ -4,21 +4,24 @@
 //   log probabilities:  dx = p (-g - u (log p + H)), + g at the given class
 //   distillation:       q = softmax(scale t) of the teacher's entries;  loss = sum q (log q - log p);  dx = g scale (p - sum of q at the column)
 //
-// One pass over a row has its maximum and sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end.  The gradient
-// reads the row again, from the caches, and writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.
+// Rows of up to 2048 columns lie in the registers of a part of a wavefront or of all of it and are read once.  One pass over a longer row has its maximum and
+// sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end; the gradient reads the row again, from the caches, and
+// writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.
 #include "heads.hpp"
+#include "mx_parts.hpp"
 #include "rows.hpp"
 
 namespace maxk {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256;  // of a workgroup; T below: 256 or 1024
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr float kFar = 256.f;  // 2^-256 is 0 in fp32: a difference past it need not be told, and is cut so that 0 times it stays 0
 
 // Of a part of a row: its largest value (the lowest fp32 value where it has none above), S and T.  -Inf adds 0, NaN and +Inf make S a NaN.
 struct Sums { float m, S, T; };
-__device__ __forceinline__ Sums no_sums() { return {-3.402823466e38f, 0.f, 0.f}; }
+constexpr float kLowest = -3.402823466e38f;
+__device__ __forceinline__ Sums no_sums() { return {kLowest, 0.f, 0.f}; }
 
 __device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2f(d); }
 
@@ -73,14 +76,13 @@ __device__ __forceinline__ Sums join_lanes(Sums a, float c)
     return a;
 }
 
+template <int T>
 __device__ __forceinline__ Sums join_workgroup(Sums a, float c, Sums* room)  // (passes a barrier, room is free behind the next one)
 {
     a = join_lanes<kWave>(a, c);
     if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = a;
     __syncthreads();
-    a = room[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) a = join(a, room[i], c);
+    a = join_lanes<T / kWave>(room[threadIdx.x % (T / kWave)], c);
     return a;
 }
 
@@ -100,27 +102,54 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
 }
 __device__ __forceinline__ uint64_t greater_key(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-__device__ __forceinline__ uint64_t exchange(uint64_t k, int lane, int step, bool falling)
+// of lane ^ STEP
+template <int STEP>
+__device__ __forceinline__ uint32_t across(uint32_t x)
 {
-    const uint64_t o = lane_key(k, lane ^ step);
-    return (((lane & step) == 0) == falling) == (k > o) ? k : o;
+    if constexpr (STEP == 4) x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true), x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x1B, 0xF, 0xF, true);  // row_half_mirror, quad_perm [3,2,1,0]
+    else if constexpr (STEP == 8) x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true);  // row_ror:8
+    else x = xor_lane(x, std::integral_constant<int, STEP>{});
+    return x;
+}
+template <int STEP>
+__device__ __forceinline__ uint64_t exchange(uint64_t k, int lane, bool falling)
+{
+    const uint64_t o = (uint64_t)across<STEP>((uint32_t)(k >> 32)) << 32 | across<STEP>((uint32_t)k);
+    return (((lane & STEP) == 0) == falling) == (k > o) ? k : o;
+}
+// runs of 2 STEP lanes whose halves are in opposite orders into order, falling where (lane & RUN) is 0
+template <int STEP, int RUN>
+__device__ __forceinline__ uint64_t settle(uint64_t k, int lane)
+{
+    k = exchange<STEP>(k, lane, (lane & RUN) == 0);
+    if constexpr (STEP > 1) k = settle<STEP / 2, RUN>(k, lane);
+    return k;
 }
 // keys of the 64 lanes in falling order (equal ones only where both are 0)
 __device__ __forceinline__ uint64_t sort_keys(uint64_t k, int lane)
 {
-#pragma unroll
-    for (int size = 2; size <= kWave; size *= 2)
-#pragma unroll
-        for (int step = size / 2; step > 0; step /= 2) k = exchange(k, lane, step, (lane & size) == 0);
-    return k;
+    k = settle<1, 2>(k, lane);
+    k = settle<2, 4>(k, lane);
+    k = settle<4, 8>(k, lane);
+    k = settle<8, 16>(k, lane);
+    k = settle<16, 32>(k, lane);
+    return settle<32, 64>(k, lane);
 }
 // the 64 greatest of two sets in falling order, in falling order
 __device__ __forceinline__ uint64_t merge_keys(uint64_t a, uint64_t b, int lane)
 {
-    uint64_t k = greater_key(a, lane_key(b, 63 - lane));
-#pragma unroll
-    for (int step = kWave / 2; step > 0; step /= 2) k = exchange(k, lane, step, true);
-    return k;
+    return settle<32, 64>(greater_key(a, lane_key(b, 63 - lane)), lane);
+}
+// of the wavefronts of a workgroup, for the first of them (keys: 64 of each, written)
+template <int T>
+__device__ __forceinline__ uint64_t merge_waves(uint64_t mine, uint64_t (*keys)[2 * kWave], int lane, int wave)
+{
+    for (int step = 1; step < T / kWave; step *= 2) {
+        keys[wave][lane] = mine;
+        __syncthreads();
+        if (wave % (2 * step) == 0) mine = merge_keys(mine, keys[wave + step][lane], lane);
+    }
+    return mine;
 }
 
 // A wavefront's greatest keys: in falling order over the lanes, and those that wait in LDS to be sorted in.  A unit whose largest value is below the k-th
@@ -147,19 +176,22 @@ struct Likeliest {
     }
     __device__ void sort_in()
     {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_fence();
         const int n = min(waiting, kWave), from = waiting - n;
         const uint64_t key = lane < n ? wait[from + lane] : 0;
         waiting = from;
         mine = merge_keys(mine, sort_keys(key, lane), lane);
         raise(lane_key(mine, k - 1));
     }
-    // a unit at column `col`: all lanes come here, those without columns with valid < 1
-    __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid, bool first)
+    // The k-th greatest of the lanes' largest values is no less than the k-th greatest value of all: a first bound, before anything is offered.
+    // (some: the lane has one)
+    __device__ __forceinline__ void expect(float top, bool some)
     {
-        if (first) raise((uint64_t)(uint32_t)(lane_key(sort_keys((uint64_t)(valid > 0 ? value_key(top) : 0u) << 32, lane), k - 1) >> 32) << 32);
+        raise((uint64_t)(uint32_t)(lane_key(sort_keys((uint64_t)(some ? value_key(top) : 0u) << 32, lane), k - 1) >> 32) << 32);
+    }
+    // a unit at column `col`: all lanes come here, those without columns with valid < 1
+    __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid)
+    {
         if (!__any(valid > 0 && top >= least_value)) return;
 #pragma unroll 1
         for (int j = 0; j < kRowUnit; ++j) {
@@ -205,37 +237,25 @@ struct Entries {  // of the teacher, in LDS
     float q[kMostEntries], x[kMostEntries];
 };
 
-// max and sum over a workgroup (two barriers)
-__device__ __forceinline__ float workgroup_max(float x, float* room)
+constexpr auto kMax = [](float a, float b) { return fmaxf(a, b); };
+
+template <int T, typename F>
+__device__ __forceinline__ float over_workgroup(float x, float* room, F&& f)  // (two barriers)
 {
-    x = over_lanes<kWave>(x, [](float a, float b) { return fmaxf(a, b); });
+    x = over_lanes<kWave>(x, f);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
     __syncthreads();
-    x = room[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = fmaxf(x, room[i]);
-    return x;
-}
-__device__ __forceinline__ float workgroup_sum(float x, float* room)
-{
-    x = over_lanes<kWave>(x, kAdd);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
-    __syncthreads();
-    x = room[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x += room[i];
-    return x;
+    return over_lanes<T / kWave>(room[threadIdx.x % (T / kWave)], f);
 }
 
 // The teacher's entries of a row, their q and the student's x there.  An entry whose column lies outside the row is none.
-template <int VT>
+template <int VT, int T>
 __device__ Asked take_entries(const ClassCall& C, int64_t row, Entries& E, float* room)
 {
     const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
-    float top = -3.402823466e38f, ref = -3.402823466e38f;
-    for (int i = threadIdx.x; i < C.k; i += kThreads) {
+    float top = kLowest, ref = kLowest;
+    for (int i = threadIdx.x; i < C.k; i += T) {
         const int64_t col = column_of(C, row * C.k + i);
         const bool there = col >= 0 && col < C.V;
         E.col[i] = there ? (int32_t)col : -1;
@@ -244,20 +264,20 @@ __device__ Asked take_entries(const ClassCall& C, int64_t row, Entries& E, float
         top = fmaxf(top, E.q[i]);
         ref = fmaxf(ref, E.x[i]);
     }
-    top = workgroup_max(top, room);
-    ref = workgroup_max(ref, room);
+    top = over_workgroup<T>(top, room, kMax);
+    ref = over_workgroup<T>(ref, room, kMax);
     const float c = C.scale * kLog2e;
     float sum = 0.f;
-    for (int i = threadIdx.x; i < C.k; i += kThreads) sum += exp2_of((E.q[i] - top) * c);
-    sum = workgroup_sum(sum, room);
+    for (int i = threadIdx.x; i < C.k; i += T) sum += exp2_of((E.q[i] - top) * c);
+    sum = over_workgroup<T>(sum, room, kAdd);
     const float ln = logf(sum), inverse = 1.f / sum;
     float loss = 0.f;
-    for (int i = threadIdx.x; i < C.k; i += kThreads) {
+    for (int i = threadIdx.x; i < C.k; i += T) {
         const float d = (E.q[i] - top) * c, q = sum == 0.f ? 0.f : exp2_of(d) * inverse;
         if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - (E.x[i] - ref) * C.scale);
         E.q[i] = q;
     }
-    loss = workgroup_sum(loss, room);
+    loss = over_workgroup<T>(loss, room, kAdd);
     return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
 }
 
@@ -318,28 +338,47 @@ __device__ __forceinline__ Slope row_slope(const ClassCall& C, int64_t row, cons
 }
 
 // Columns [first, last) of a row by a workgroup: their sums, and the likeliest of them in every wavefront
-template <int VT, bool TOP>
+template <int VT, int T, bool TOP>
 __device__ __forceinline__ Sums sum_columns(const ClassCall& C, int64_t row, int first, int last, Likeliest& best)
 {
     using S = value_store_t<VT>;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
     const float c = C.scale * kLog2e;
     Sums sums = no_sums();
+    int base = first;
     bool begun = false;
-    for (int base = first; base < last; base += kThreads * kRowUnit) {
+    for (; base + 2 * T * kRowUnit <= last; base += 2 * T * kRowUnit) {  // two units under way
+        const int col = base + threadIdx.x * kRowUnit, next = col + T * kRowUnit;
+        float v[2][kRowUnit];
+        load_whole_unit<VT>(x + col, v[0]);
+        load_whole_unit<VT>(x + next, v[1]);
+        const float top = largest(v[0]), other = largest(v[1]);
+        absorb(sums, v[0], top, c);
+        absorb(sums, v[1], other, c);
+        if constexpr (TOP) {
+            if (!begun) best.expect(fmaxf(top, other), true);
+            begun = true;
+            best.offer(v[0], top, col, kRowUnit);
+            best.offer(v[1], other, next, kRowUnit);
+        }
+    }
+    for (; base < last; base += T * kRowUnit) {
         const int col = base + threadIdx.x * kRowUnit;
         float v[kRowUnit];
         load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
         const float top = largest(v);
         absorb(sums, v, top, c);
-        if constexpr (TOP) best.offer(v, top, col, last - col, !begun);
-        begun = true;
+        if constexpr (TOP) {
+            if (!begun) best.expect(top, col < last);
+            begun = true;
+            best.offer(v, top, col, last - col);
+        }
     }
     return sums;
 }
 
 // Their gradient; distillation's entries in these columns follow
-template <int VT, bool DISTILL>
+template <int VT, int T, bool DISTILL>
 __device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
 {
     using S = value_store_t<VT>;
@@ -350,22 +389,36 @@ __device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, 
         const float d = fmaxf((v - s.m) * c, -kFar);
         return exp2_of(d) * (DISTILL ? k.A : fmaf(k.B, d, k.A));
     };
-    for (int base = first; base < last; base += kThreads * kRowUnit) {
-        const int col = base + threadIdx.x * kRowUnit;
-        if (col >= last) break;
-        float v[kRowUnit];
-        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
+    const auto unit = [&](float (&v)[kRowUnit], int col) {
 #pragma unroll
         for (int j = 0; j < kRowUnit; ++j) v[j] = slope(v[j]);
         if (!DISTILL && (uint64_t)(k.y - col) < kRowUnit) {
 #pragma unroll
             for (int j = 0; j < kRowUnit; ++j) v[j] += j == (int)(k.y - col) ? k.g : 0.f;
         }
+    };
+    int base = first;
+    for (; base + 2 * T * kRowUnit <= last; base += 2 * T * kRowUnit) {
+        const int col = base + threadIdx.x * kRowUnit, next = col + T * kRowUnit;
+        float v[2][kRowUnit];
+        load_whole_unit<VT>(x + col, v[0]);
+        load_whole_unit<VT>(x + next, v[1]);
+        unit(v[0], col);
+        store_whole_unit<VT>(dx + col, v[0]);
+        unit(v[1], next);
+        store_whole_unit<VT>(dx + next, v[1]);
+    }
+    for (; base < last; base += T * kRowUnit) {
+        const int col = base + threadIdx.x * kRowUnit;
+        if (col >= last) break;
+        float v[kRowUnit];
+        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
+        unit(v, col);
         store_row_unit<VT>(dx + col, last - col, v);
     }
     if constexpr (DISTILL) {
         __syncthreads();  // what is stored above at their columns is stored again
-        for (int i = threadIdx.x; i < C.k; i += kThreads) {
+        for (int i = threadIdx.x; i < C.k; i += T) {
             const int col = E->col[i];
             if (col < first || col >= last) continue;
             float q = 0.f;
@@ -380,38 +433,212 @@ __device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, 
     }
 }
 
-// A workgroup a row
-template <int VT, bool DISTILL, bool GRAD, bool TOP>
-__global__ void __launch_bounds__(kThreads) class_rows_kernel(ClassCall C)
+// ---- a row in the registers of L lanes, U units of 8 columns each ----
+
+// The k greatest of the L lanes' keys, in turn: a key is a double in [1, 2) whose last 20 bits hold the column, so that the greatest is one operation
+// a step; rows are of at most 2048 columns.  A key that was taken is below 1.
+__device__ __forceinline__ double pair_key(float x, int col)
 {
-    __shared__ Sums sums_room[kWaves];
-    __shared__ float room[kWaves];
+    const uint32_t v = value_key(x);
+    return __hiloint2double((int)(0x3FF00000u | v >> 12), (int)(v << 20 | (0xFFFFFu - (uint32_t)col)));
+}
+__device__ __forceinline__ uint64_t unpaired(double key)
+{
+    const uint32_t high = (uint32_t)__double2hiint(key), low = (uint32_t)__double2loint(key);
+    return high < 0x3FF00000u ? 0 : (uint64_t)(high << 12 | low >> 20) << 32 | (0xFFFFFFFFu - (0xFFFFFu - (low & 0xFFFFFu)));
+}
+
+// Entries of the teacher: the loss's part, and (GRAD) the sums of q at every column to `spread`, LDS for the columns of the row
+template <int VT, int L, int U, bool GRAD>
+__device__ __forceinline__ Asked team_entries(const ClassCall& C, int64_t row, int lane, float* spread)
+{
+    const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
+    const float c = C.scale * kLog2e;
+    const auto column = [&](int i) {
+        const int64_t col = column_of(C, row * C.k + i);
+        return col >= 0 && col < C.V ? (int)col : -1;
+    };
+    const auto value = [&](int i, int col) { return col >= 0 ? teacher_value(C, row * C.k + i) : -__builtin_inff(); };
+    float top = kLowest, ref = kLowest;
+    for (int i = lane; i < C.k; i += L) {
+        const int col = column(i);
+        top = fmaxf(top, value(i, col));
+        if (col >= 0) ref = fmaxf(ref, widen_value<VT>(x[col]));
+    }
+    top = over_lanes<L>(top, kMax);
+    ref = over_lanes<L>(ref, kMax);
+    float sum = 0.f;
+    for (int i = lane; i < C.k; i += L) sum += exp2_of((value(i, column(i)) - top) * c);
+    sum = over_lanes<L>(sum, kAdd);
+    const float ln = logf(sum), inverse = 1.f / sum;
+    const auto weight = [&](float d) { return sum == 0.f ? 0.f : exp2_of(d) * inverse; };
+    if constexpr (GRAD) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < kRowUnit; j += 4) *reinterpret_cast<float4*>(spread + (lane + u * L) * kRowUnit + j) = make_float4(0.f, 0.f, 0.f, 0.f);
+        wave_fence();
+        for (int i = lane; i < C.k; i += L)
+            if (const int col = column(i); col >= 0) spread[col] = __int_as_float(i + 1);  // (whose entry is to write there: one of them where there are several)
+        wave_fence();
+    }
+    float loss = 0.f;
+    bool several = false;
+    for (int i = lane; i < C.k; i += L) {
+        const int col = column(i);
+        const float d = (value(i, col) - top) * c, q = weight(d);
+        if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - ((col >= 0 ? widen_value<VT>(x[col]) : -__builtin_inff()) - ref) * C.scale);
+        if constexpr (GRAD) several |= col >= 0 && __float_as_int(spread[col]) != i + 1;
+    }
+    if constexpr (GRAD) {
+        // (all lanes' marks are read before the first sum is written)
+        several = over_lanes<L>((uint32_t)several, [](uint32_t a, uint32_t b) { return a | b; });
+        wave_fence();
+        for (int i = lane; i < C.k; i += L) {
+            const int col = column(i);
+            if (col < 0) continue;
+            float q = 0.f;
+            if (several) {  // sums in the entries' order
+                if (__float_as_int(spread[col]) != i + 1) continue;
+                for (int j = 0; j < C.k; ++j)
+                    if (column(j) == col) q += weight((value(j, col) - top) * c);
+            } else {
+                q = weight((value(i, col) - top) * c);
+            }
+            spread[col] = q;
+        }
+        wave_fence();
+    }
+    return {0.f, over_lanes<L>(loss, kAdd), ref, sum == 0.f ? 0.f : sum * inverse};
+}
+
+template <int VT, int L, int U, bool DISTILL, bool GRAD, bool TOP>
+__global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
+{
+    using S = value_store_t<VT>;
+    constexpr int kTeams = kThreads / L;
+    __shared__ __attribute__((aligned(16))) float spread[DISTILL && GRAD ? kTeams * L * U * kRowUnit : 1];
+    __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? 2 * kWave : 1];
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    if (row >= C.N) return;
+    const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
+    const float c = C.scale * kLog2e;
+    float v[U][kRowUnit];
+    Sums s = no_sums();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int col = (lane + u * L) * kRowUnit;
+        load_row_unit<VT>(x + col, C.V - col, end, -__builtin_inff(), v[u]);
+    }
+    float* mine = spread + (DISTILL && GRAD ? team * L * U * kRowUnit : 0);
+    Asked asked;
+    if constexpr (DISTILL) asked = team_entries<VT, L, U, GRAD>(C, row, lane, mine);
+    else asked = given_class<VT>(C, row);
+    float lane_top = largest(v[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u) lane_top = fmaxf(lane_top, largest(v[u]));
+    s.m = over_lanes<L>(fmaxf(lane_top, kLowest), kMax);
+    float e[U][kRowUnit];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) {
+            const float d = (v[u][j] - s.m) * c;
+            e[u][j] = exp2_of(d);
+            s.S += e[u][j];
+            if constexpr (!DISTILL) s.T = fmaf(e[u][j], fmaxf(d, -kFar), s.T);
+        }
+    s.S = over_lanes<L>(s.S, kAdd);
+    if constexpr (!DISTILL) s.T = over_lanes<L>(s.T, kAdd);
+    const Found f = row_results(C, row, s, asked);
+    if (lane == 0) store_results(C, row, f);
+    if constexpr (TOP && L == kWave) {
+        Likeliest best;
+        best.begin(C.top_k, keys[team], lane);
+        best.expect(lane_top, lane * kRowUnit < C.V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (lane + u * L) * kRowUnit;
+            best.offer(v[u], largest(v[u]), col, C.V - col);
+        }
+        best.end();
+        store_likeliest(C, row, s, f.ln, best.mine, lane);
+    } else if constexpr (TOP) {
+        static_assert(U == 1);
+        double key[kRowUnit];
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) key[j] = lane * kRowUnit + j < C.V ? pair_key(v[0][j], lane * kRowUnit + j) : 0.0;
+        double taken = 0.0;
+        for (int i = 0; i < C.top_k; ++i) {
+            double best = key[0];
+#pragma unroll
+            for (int j = 1; j < kRowUnit; ++j) best = fmax(best, key[j]);
+            best = over_lanes<L>(best, [](double a, double b) { return fmax(a, b); });
+            const int col = (int)(0xFFFFFu - ((uint32_t)__double2loint(best) & 0xFFFFFu));
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j)
+                if (col == lane * kRowUnit + j) key[j] = __hiloint2double(0, __double2loint(key[j]));
+            if (i % L == lane) taken = best;
+            if (i % L == L - 1 || i == C.top_k - 1) {
+                const int at = i - i % L + lane;
+                if (at <= i) store_likeliest(C, row, s, f.ln, unpaired(taken), at);
+            }
+        }
+    }
+    if constexpr (GRAD) {
+        const Slope k = row_slope(C, row, s, asked, f);
+        S* dx = (S*)C.dlogits + row * C.V;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (lane + u * L) * kRowUnit;
+            float g[kRowUnit];
+            if constexpr (DISTILL) {
+                const float4 a = *reinterpret_cast<const float4*>(mine + col), b = *reinterpret_cast<const float4*>(mine + col + 4);
+                const float q[kRowUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < kRowUnit; ++j) g[j] = fmaf(-k.g, q[j], e[u][j] * k.A);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kRowUnit; ++j) {
+                    g[j] = e[u][j] * fmaf(k.B, fmaxf((v[u][j] - s.m) * c, -kFar), k.A);
+                    if (k.y == col + j) g[j] += k.g;
+                }
+            }
+            store_row_unit<VT>(dx + col, C.V - col, g);
+        }
+    }
+}
+
+// ---- a workgroup a row ----
+
+template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
+__global__ void __launch_bounds__(T) class_rows_kernel(ClassCall C)
+{
+    __shared__ Sums sums_room[T / kWave];
+    __shared__ float room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
-    __shared__ uint64_t keys[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     Likeliest best;
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
     Asked asked;
-    if constexpr (DISTILL) asked = take_entries<VT>(C, row, entries, room);
+    if constexpr (DISTILL) asked = take_entries<VT, T>(C, row, entries, room);
     else asked = given_class<VT>(C, row);
-    Sums s = sum_columns<VT, TOP>(C, row, 0, C.V, best);
-    s = join_workgroup(s, C.scale * kLog2e, sums_room);
+    Sums s = sum_columns<VT, T, TOP>(C, row, 0, C.V, best);
+    s = join_workgroup<T>(s, C.scale * kLog2e, sums_room);
     const Found f = row_results(C, row, s, asked);
     if constexpr (TOP) {
         best.end();
-        keys[wave][lane] = best.mine;
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < kWaves; ++w) best.mine = merge_keys(best.mine, keys[w][lane], lane);
-            store_likeliest(C, row, s, f.ln, best.mine, lane);
-        }
+        const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
+        if (wave == 0) store_likeliest(C, row, s, f.ln, key, lane);
     }
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (GRAD) {
         const Slope k = row_slope(C, row, s, asked, f);
-        if constexpr (DISTILL) store_gradient<VT, true>(C, row, 0, C.V, s, k, &entries);
-        else store_gradient<VT, false>(C, row, 0, C.V, s, k, nullptr);
+        if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, 0, C.V, s, k, &entries);
+        else store_gradient<VT, T, false>(C, row, 0, C.V, s, k, nullptr);
     }
 }
 
@@ -427,10 +654,11 @@ struct Parts {
 template <int VT, bool DISTILL, bool TOP>
 __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Parts P)
 {
-    __shared__ Sums sums_room[kWaves];
-    __shared__ float room[kWaves];
+    constexpr int T = kThreads;
+    __shared__ Sums sums_room[T / kWave];
+    __shared__ float room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
-    __shared__ uint64_t keys[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
     const int64_t row = blockIdx.x / P.segments;
     const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
@@ -438,50 +666,45 @@ __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Part
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
     if (segment == 0) {
         Asked asked;
-        if constexpr (DISTILL) asked = take_entries<VT>(C, row, entries, room);
+        if constexpr (DISTILL) asked = take_entries<VT, T>(C, row, entries, room);
         else asked = given_class<VT>(C, row);
         if (threadIdx.x == 0) P.asked[row] = asked;
     }
-    Sums s = sum_columns<VT, TOP>(C, row, first, last, best);
-    s = join_workgroup(s, C.scale * kLog2e, sums_room);
+    Sums s = sum_columns<VT, T, TOP>(C, row, first, last, best);
+    s = join_workgroup<T>(s, C.scale * kLog2e, sums_room);
     if (threadIdx.x == 0) P.sums[blockIdx.x] = s;
     if constexpr (TOP) {
         best.end();
-        keys[wave][lane] = best.mine;
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < kWaves; ++w) best.mine = merge_keys(best.mine, keys[w][lane], lane);
-            if (lane < C.top_k) P.keys[(int64_t)blockIdx.x * C.top_k + lane] = best.mine;
-        }
+        const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
+        if (wave == 0 && lane < C.top_k) P.keys[(int64_t)blockIdx.x * C.top_k + lane] = key;
     }
 }
 
+template <int T>
 __device__ __forceinline__ Sums join_segments(const ClassCall& C, const Parts& P, int64_t row, Sums* room)
 {
     Sums s = no_sums();
-    for (int i = threadIdx.x; i < P.segments; i += kThreads) s = join(s, P.sums[row * P.segments + i], C.scale * kLog2e);
-    return join_workgroup(s, C.scale * kLog2e, room);
+    for (int i = threadIdx.x; i < P.segments; i += T) s = join(s, P.sums[row * P.segments + i], C.scale * kLog2e);
+    return join_workgroup<T>(s, C.scale * kLog2e, room);
 }
 
-template <bool TOP>
-__global__ void __launch_bounds__(kThreads) class_join_kernel(ClassCall C, Parts P)
+template <int T, bool TOP>
+__global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
 {
-    __shared__ Sums sums_room[kWaves];
-    __shared__ uint64_t keys[kWaves][kWave];
+    __shared__ Sums sums_room[T / kWave];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
-    const Sums s = join_segments(C, P, row, sums_room);
+    uint64_t mine = 0;
+    if constexpr (TOP) {
+        for (int i = wave; i < P.segments; i += T / kWave)
+            mine = merge_keys(mine, lane < C.top_k ? P.keys[(row * P.segments + i) * C.top_k + lane] : 0, lane);
+    }
+    const Sums s = join_segments<T>(C, P, row, sums_room);
     const Found f = row_results(C, row, s, P.asked[row]);
     if constexpr (TOP) {
-        uint64_t mine = 0;
-        for (int i = wave; i < P.segments; i += kWaves)
-            mine = merge_keys(mine, lane < C.top_k ? P.keys[(row * P.segments + i) * C.top_k + lane] : 0, lane);
-        keys[wave][lane] = mine;
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < kWaves; ++w) mine = merge_keys(mine, keys[w][lane], lane);
-            store_likeliest(C, row, s, f.ln, mine, lane);
-        }
+        mine = merge_waves<T>(mine, keys, lane, wave);
+        if (wave == 0) store_likeliest(C, row, s, f.ln, mine, lane);
     }
     if (threadIdx.x == 0) store_results(C, row, f);
 }
@@ -489,20 +712,24 @@ __global__ void __launch_bounds__(kThreads) class_join_kernel(ClassCall C, Parts
 template <int VT, bool DISTILL>
 __global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, Parts P)
 {
-    __shared__ Sums sums_room[kWaves];
-    __shared__ float room[kWaves];
+    constexpr int T = kThreads;
+    __shared__ Sums sums_room[T / kWave];
+    __shared__ float room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     const int64_t row = blockIdx.x / P.segments;
     const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
-    const Sums s = join_segments(C, P, row, sums_room);
+    const Sums s = join_segments<T>(C, P, row, sums_room);
     const Asked asked = P.asked[row];
-    if constexpr (DISTILL) take_entries<VT>(C, row, entries, room);  // (x of other segments may have been overwritten: only those of this one are used)
+    if constexpr (DISTILL) take_entries<VT, T>(C, row, entries, room);  // (x of other segments may have been overwritten: only those of this one are used)
     const Found f = row_results(C, row, s, asked);
     if (segment == 0 && threadIdx.x == 0) store_results(C, row, f);
     const Slope k = row_slope(C, row, s, asked, f);
-    if constexpr (DISTILL) store_gradient<VT, true>(C, row, first, last, s, k, &entries);
-    else store_gradient<VT, false>(C, row, first, last, s, k, nullptr);
+    if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, first, last, s, k, &entries);
+    else store_gradient<VT, T, false>(C, row, first, last, s, k, nullptr);
 }
+
+// Rows of so many columns take workgroups of 1024 threads
+constexpr int kWideRow = 16384;
 
 // Segments of a row
 struct Cut { int segments, width; };
@@ -518,16 +745,36 @@ Cut cut_of(int64_t N, int V)
 
 int64_t up16(int64_t n) { return (n + 15) & ~15ll; }
 
+template <int VT, int L, int U, bool DISTILL, bool GRAD, bool TOP>
+maxk_status run_teams(const ClassCall& C, hipStream_t s)
+{
+    constexpr int kTeams = kThreads / L;
+    hipLaunchKernelGGL((class_team_kernel<VT, L, U, DISTILL, GRAD, TOP>), dim3((unsigned)((C.N + kTeams - 1) / kTeams)), dim3(kThreads), 0, s, C);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
+template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
+maxk_status run_rows(const ClassCall& C, hipStream_t s)
+{
+    hipLaunchKernelGGL((class_rows_kernel<VT, T, DISTILL, GRAD, TOP>), dim3((unsigned)C.N), dim3(T), 0, s, C);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
 template <int VT, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
 {
+    const int units = (C.V + kRowUnit - 1) / kRowUnit;
+    if (units <= 4) return run_teams<VT, 4, 1, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 8) return run_teams<VT, 8, 1, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 16) return run_teams<VT, 16, 1, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 32) return run_teams<VT, 32, 1, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 64) return run_teams<VT, 64, 1, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 128) return run_teams<VT, 64, 2, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
-    if (cut.segments == 1) {
-        if (C.N > 0x7FFFFFFF) return MAXK_UNSUPPORTED;
-        hipLaunchKernelGGL((class_rows_kernel<VT, DISTILL, GRAD, TOP>), dim3((unsigned)C.N), dim3(kThreads), 0, s, C);
-        MAXK_LAUNCH_CHECK();
-        return MAXK_OK;
-    }
+    if (cut.segments == 1) return C.V >= kWideRow ? run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s) : run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);
     char* at = (char*)workspace;
     Parts P = {cut.segments, cut.width, (Sums*)at, nullptr, nullptr};
     at += up16(C.N * cut.segments * (int64_t)sizeof(Sums));
@@ -538,7 +785,7 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     hipLaunchKernelGGL((class_parts_kernel<VT, DISTILL, TOP>), dim3(groups), dim3(kThreads), 0, s, C, P);
     MAXK_LAUNCH_CHECK();
     if constexpr (GRAD) hipLaunchKernelGGL((class_gradient_kernel<VT, DISTILL>), dim3(groups), dim3(kThreads), 0, s, C, P);
-    else hipLaunchKernelGGL((class_join_kernel<TOP>), dim3((unsigned)C.N), dim3(kThreads), 0, s, C, P);
+    else hipLaunchKernelGGL((class_join_kernel<TOP ? 1024 : kThreads, TOP>), dim3((unsigned)C.N), dim3(TOP ? 1024 : kThreads), 0, s, C, P);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }

@@ -45,17 +45,32 @@ __device__ __forceinline__ float raw_value(const RawUnit<VT>& u, int j)  // j: a
     }
 }
 
+template <int VT>
+__device__ __forceinline__ void load_whole_unit(const value_store_t<VT>* p, float (&x)[kRowUnit])
+{
+    RawUnit<VT> u;
+    u.w[0] = read16(p);
+    if constexpr (VT == MAXK_VALUE_F32) u.w[1] = read16(p + 4);
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) x[j] = raw_value<VT>(u, j);
+}
+
+template <int VT>
+__device__ __forceinline__ void store_whole_unit(value_store_t<VT>* p, const float (&x)[kRowUnit])
+{
+    value_store_t<VT> v[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) v[j] = round_value<VT>(x[j]);
+    __builtin_memcpy(p, v, sizeof(v));
+}
+
 // Unit at p, of which `valid` columns (less than 1: none) belong to the row; the others come out as `fill`.  What lies behind a row is read where it
 // belongs to the matrix, which ends at `end`.
 template <int VT>
 __device__ __forceinline__ void load_row_unit(const value_store_t<VT>* p, int valid, const value_store_t<VT>* end, float fill, float (&x)[kRowUnit])
 {
     if (valid > 0 && p + kRowUnit <= end) {
-        RawUnit<VT> u;
-        u.w[0] = read16(p);
-        if constexpr (VT == MAXK_VALUE_F32) u.w[1] = read16(p + 4);
-#pragma unroll
-        for (int j = 0; j < kRowUnit; ++j) x[j] = raw_value<VT>(u, j);
+        load_whole_unit<VT>(p, x);
         if (valid < kRowUnit) {
 #pragma unroll
             for (int j = 1; j < kRowUnit; ++j) x[j] = j < valid ? x[j] : fill;
