@@ -524,17 +524,20 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     if (row >= C.N) return;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
     const float c = C.scale * kLog2e;
-    float v[U][kRowUnit];
-    Sums s = no_sums();
+    RawUnit<VT> raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int col = (lane + u * L) * kRowUnit;
-        load_row_unit<VT>(x + col, C.V - col, end, -__builtin_inff(), v[u]);
+        raw[u] = fetch_row_unit<VT>(x + col, C.V - col, end);
     }
     float* mine = spread + (DISTILL && GRAD ? team * L * U * kRowUnit : 0);
     Asked asked;
     if constexpr (DISTILL) asked = team_entries<VT, L, U, GRAD>(C, row, lane, mine);
     else asked = given_class<VT>(C, row);
+    float v[U][kRowUnit];
+#pragma unroll
+    for (int u = 0; u < U; ++u) unit_values<VT>(raw[u], C.V - (lane + u * L) * kRowUnit, -__builtin_inff(), v[u]);
+    Sums s = no_sums();
     float lane_top = largest(v[0]);
 #pragma unroll
     for (int u = 1; u < U; ++u) lane_top = fmaxf(lane_top, largest(v[u]));

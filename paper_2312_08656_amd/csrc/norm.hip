@@ -34,17 +34,20 @@ __global__ void __launch_bounds__(norm_threads(L)) norm_kernel(NormCall C, int64
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / L; row < N; row += (int64_t)gridDim.x * kTeams, turn ^= 1) {
         float h[U][kRowUnit];
+        RawUnit<VT> raw[U], added[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (lane + u * L) * kRowUnit;
-            load_row_unit<VT>(X + row * dim + col, dim - col, X_end, 0.f, h[u]);
+            raw[u] = fetch_row_unit<VT>(X + row * dim + col, dim - col, X_end);
+            if (R) added[u] = fetch_row_unit<VT>(R + row * dim + col, dim - col, R_end);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) unit_values<VT>(raw[u], dim - (lane + u * L) * kRowUnit, 0.f, h[u]);
         if (R) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int col = (lane + u * L) * kRowUnit;
                 float r[kRowUnit];
-                load_row_unit<VT>(R + row * dim + col, dim - col, R_end, 0.f, r);
+                unit_values<VT>(added[u], dim - (lane + u * L) * kRowUnit, 0.f, r);
 #pragma unroll
                 for (int j = 0; j < kRowUnit; ++j) h[u][j] = rounded<VT>(h[u][j] + r[j]);
             }
@@ -98,11 +101,19 @@ __global__ void __launch_bounds__(norm_threads(L)) norm_grad_kernel(NormGradCall
     for (int64_t row = (int64_t)blockIdx.x * kTeams + team; row < N; row += (int64_t)gridDim.x * kTeams, turn ^= 1) {
         float x[U][kRowUnit], dy[U][kRowUnit];
         const float rstd = C.rstd[row];
+        RawUnit<VT> raw_h[U], raw_dy[U], raw_dh[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (lane + u * L) * kRowUnit;
-            load_row_unit<VT>(H + row * dim + col, dim - col, H + N * dim, 0.f, x[u]);
-            load_row_unit<VT>(dY + row * dim + col, dim - col, dY + N * dim, 0.f, dy[u]);
+            raw_h[u] = fetch_row_unit<VT>(H + row * dim + col, dim - col, H + N * dim);
+            raw_dy[u] = fetch_row_unit<VT>(dY + row * dim + col, dim - col, dY + N * dim);
+            if (dH) raw_dh[u] = fetch_row_unit<VT>(dH + row * dim + col, dim - col, dH + N * dim);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int valid = dim - (lane + u * L) * kRowUnit;
+            unit_values<VT>(raw_h[u], valid, 0.f, x[u]);
+            unit_values<VT>(raw_dy[u], valid, 0.f, dy[u]);
         }
         float dot = 0.f;
 #pragma unroll
@@ -119,7 +130,7 @@ __global__ void __launch_bounds__(norm_threads(L)) norm_grad_kernel(NormGradCall
         for (int u = 0; u < U; ++u) {
             const int col = (lane + u * L) * kRowUnit;
             float dh[kRowUnit] = {};
-            if (dH) load_row_unit<VT>(dH + row * dim + col, dim - col, dH + N * dim, 0.f, dh);
+            if (dH) unit_values<VT>(raw_dh[u], dim - col, 0.f, dh);
             float dx[kRowUnit];
 #pragma unroll
             for (int j = 0; j < kRowUnit; ++j) dx[j] = fmaf(rstd, fmaf(-dot, x[u][j], dy[u][j]), dh[j]);
@@ -149,20 +160,23 @@ __global__ void __launch_bounds__(norm_threads(L)) norm_grad_kernel(NormGradCall
     }
 }
 
-// dgamma of the workgroups' sums: 16 columns and 16 ranges of them a workgroup
-__global__ void __launch_bounds__(kThreads) add_parts_kernel(const float* parts, int n, int dim, float* dgamma)
+// dgamma of the workgroups' sums: 16 columns and 64 ranges of them a workgroup
+constexpr int kRanges = 64;
+__global__ void __launch_bounds__(16 * kRanges) add_parts_kernel(const float* parts, int n, int dim, float* dgamma)
 {
-    __shared__ double room[16][17];
+    __shared__ double room[kRanges][17];
     const int c = threadIdx.x & 15, at = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     double sum = 0.0;
-    if (col < dim)
-        for (int i = at; i < n; i += 16) sum += (double)parts[(int64_t)i * dim + col];
-    room[at][c] = sum;
-    __syncthreads();
-    if (at == 0 && col < dim) {
-        for (int i = 1; i < 16; ++i) sum += room[i][c];
-        dgamma[col] = (float)sum;
+    if (col < dim) {
+#pragma unroll 8
+        for (int i = at; i < n; i += kRanges) sum += (double)parts[(int64_t)i * dim + col];
     }
+    room[at][c] = sum;
+    for (int half = kRanges / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (at < half) room[at][c] += room[at + half][c];
+    }
+    if (at == 0 && col < dim) dgamma[col] = (float)room[0][c];
 }
 
 // Lanes of a row and units of a lane: of the forms below the one with the fewest lanes and units that a row fills
@@ -200,19 +214,27 @@ maxk_status with_form(const RowForm& f, F&& call)
     return MAXK_UNSUPPORTED;
 }
 
-constexpr int kMostGroups = 2048, kMostGradGroups = 1024;
+constexpr int kMostGroups = 8192;
 
-int64_t groups_for(int64_t N, int dim, int most)
+int64_t norm_groups(int64_t N, int dim)
 {
     const int teams = teams_of(row_form(dim));
-    return std::min<int64_t>((N + teams - 1) / teams, most);
+    return std::min<int64_t>((N + teams - 1) / teams, kMostGroups);
+}
+
+// The gradient's leave a row of dim sums each: 8 rows for each, so that these are few beside them, and four of 256 threads on a CU at most.
+int64_t grad_groups(int64_t N, int dim)
+{
+    const int teams = teams_of(row_form(dim));
+    const int64_t all = (N + teams - 1) / teams, resident = 4 * 256 * kThreads / norm_threads(row_form(dim).lanes);
+    return std::min({all, resident, std::max<int64_t>(256, N / 8)});
 }
 
 template <int VT>
 maxk_status norm(const NormCall& C, int64_t N, int dim, hipStream_t s)
 {
     return with_form(row_form(dim), [&](auto L, auto U) -> maxk_status {
-        hipLaunchKernelGGL((norm_kernel<VT, L.value, U.value>), dim3((unsigned)groups_for(N, dim, kMostGroups)), dim3(norm_threads(L.value)), 0, s, C, N, dim);
+        hipLaunchKernelGGL((norm_kernel<VT, L.value, U.value>), dim3((unsigned)norm_groups(N, dim)), dim3(norm_threads(L.value)), 0, s, C, N, dim);
         MAXK_LAUNCH_CHECK();
         return MAXK_OK;
     });
@@ -221,7 +243,7 @@ maxk_status norm(const NormCall& C, int64_t N, int dim, hipStream_t s)
 template <int VT>
 maxk_status norm_grad(const NormGradCall& C, int64_t N, int dim, hipStream_t s)
 {
-    const int64_t groups = groups_for(N, dim, kMostGradGroups);
+    const int64_t groups = grad_groups(N, dim);
     float* parts = !C.dgamma ? nullptr : groups == 1 ? C.dgamma : C.workspace;
     const maxk_status st = with_form(row_form(dim), [&](auto L, auto U) -> maxk_status {
         hipLaunchKernelGGL((norm_grad_kernel<VT, L.value, U.value>), dim3((unsigned)groups), dim3(norm_threads(L.value)), 0, s, C, parts, N, dim);
@@ -229,7 +251,7 @@ maxk_status norm_grad(const NormGradCall& C, int64_t N, int dim, hipStream_t s)
         return MAXK_OK;
     });
     if (st != MAXK_OK || !C.dgamma || groups == 1) return st;
-    hipLaunchKernelGGL(add_parts_kernel, dim3((dim + 15) / 16), dim3(kThreads), 0, s, parts, (int)groups, dim, C.dgamma);
+    hipLaunchKernelGGL(add_parts_kernel, dim3((dim + 15) / 16), dim3(16 * kRanges), 0, s, parts, (int)groups, dim, C.dgamma);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
@@ -245,7 +267,7 @@ maxk_status launch_rms_norm(const NormCall& C, int value_type, int64_t N, int di
 
 int64_t rms_norm_grad_workspace(int64_t N, int dim)
 {
-    return std::max<int64_t>(16, N == 0 ? 0 : groups_for(N, dim, kMostGradGroups) * dim * (int64_t)sizeof(float));
+    return std::max<int64_t>(16, N == 0 ? 0 : grad_groups(N, dim) * dim * (int64_t)sizeof(float));
 }
 
 maxk_status launch_rms_norm_grad(const NormGradCall& C, int value_type, int64_t N, int dim, hipStream_t s)

@@ -46,11 +46,17 @@ __device__ __forceinline__ float raw_value(const RawUnit<VT>& u, int j)  // j: a
 }
 
 template <int VT>
-__device__ __forceinline__ void load_whole_unit(const value_store_t<VT>* p, float (&x)[kRowUnit])
+__device__ __forceinline__ RawUnit<VT> whole_unit(const value_store_t<VT>* p)
 {
     RawUnit<VT> u;
     u.w[0] = read16(p);
     if constexpr (VT == MAXK_VALUE_F32) u.w[1] = read16(p + 4);
+    return u;
+}
+template <int VT>
+__device__ __forceinline__ void load_whole_unit(const value_store_t<VT>* p, float (&x)[kRowUnit])
+{
+    const RawUnit<VT> u = whole_unit<VT>(p);
 #pragma unroll
     for (int j = 0; j < kRowUnit; ++j) x[j] = raw_value<VT>(u, j);
 }
@@ -64,21 +70,33 @@ __device__ __forceinline__ void store_whole_unit(value_store_t<VT>* p, const flo
     __builtin_memcpy(p, v, sizeof(v));
 }
 
-// Unit at p, of which `valid` columns (less than 1: none) belong to the row; the others come out as `fill`.  What lies behind a row is read where it
-// belongs to the matrix, which ends at `end`.
+// Unit at p, of which `valid` columns (less than 1: none) belong to the row.  What lies behind a row is read where it belongs to the matrix, which ends at
+// `end`.  (Values are taken out apart from it: a lane's units are under way together.)
+template <int VT>
+__device__ __forceinline__ RawUnit<VT> fetch_row_unit(const value_store_t<VT>* p, int valid, const value_store_t<VT>* end)
+{
+    RawUnit<VT> u = {};
+    const bool some = valid > 0, whole = p + kRowUnit <= end;
+    if (some && whole) u = whole_unit<VT>(p);
+    if (some && !whole) {  // the matrix's last columns
+        value_store_t<VT> v[kRowUnit];
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) v[j] = j < valid ? p[j] : value_store_t<VT>(0);
+        __builtin_memcpy(&u, v, sizeof(v));
+    }
+    return u;
+}
+// its values, `fill` in the columns that do not belong to the row
+template <int VT>
+__device__ __forceinline__ void unit_values(const RawUnit<VT>& u, int valid, float fill, float (&x)[kRowUnit])
+{
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) x[j] = j < valid ? raw_value<VT>(u, j) : fill;
+}
 template <int VT>
 __device__ __forceinline__ void load_row_unit(const value_store_t<VT>* p, int valid, const value_store_t<VT>* end, float fill, float (&x)[kRowUnit])
 {
-    if (valid > 0 && p + kRowUnit <= end) {
-        load_whole_unit<VT>(p, x);
-        if (valid < kRowUnit) {
-#pragma unroll
-            for (int j = 1; j < kRowUnit; ++j) x[j] = j < valid ? x[j] : fill;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kRowUnit; ++j) x[j] = j < valid ? widen_value<VT>(p[j]) : fill;
-    }
+    unit_values<VT>(fetch_row_unit<VT>(p, valid, end), valid, fill, x);
 }
 
 template <int VT>

@@ -31,7 +31,7 @@ def check(X, codes, scales, W, bias, y_dtype):
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
 @pytest.mark.parametrize("N", [1, 2, 5, 16, 17, 40])
-@pytest.mark.parametrize("din,dout", [(1, 1), (31, 17), (32, 16), (100, 47), (256, 256), (500, 33), (512, 64), (513, 15), (1433, 100), (4096, 65), (9000, 31)])
+@pytest.mark.parametrize("din,dout", [(1, 1), (31, 17), (32, 16), (100, 47), (256, 256), (500, 33), (512, 64), (513, 15), (1433, 100), (4096, 65), (9000, 31), (16000, 20), (33000, 9), (65536, 5)])
 def test_matvec(din, dout, N, dtype):
     rng = np.random.default_rng(din + N)
     codes, scales, W = weights(rng, dout, din)
