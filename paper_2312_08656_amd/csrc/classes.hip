@@ -27,6 +27,7 @@ __device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2
 
 __device__ __forceinline__ void move_to(Sums& a, float m, float c)  // m at least a.m
 {
+#pragma clang fp contract(off)
     const float shift = fminf((m - a.m) * c, kFar), f = exp2_of(-shift);
     a.T = f * fmaf(-shift, a.S, a.T);
     a.S *= f;
@@ -41,19 +42,48 @@ __device__ __forceinline__ float largest(const float (&x)[kRowUnit])
     return m;
 }
 
-__device__ __forceinline__ void absorb(Sums& a, const float (&x)[kRowUnit], float top, float c)
-{
-    move_to(a, fmaxf(a.m, top), c);
+// A lane's sums on its way along a long row.  d = x c - q is one operation with q = m c rounded; what the rounding leaves, delta = q - m c, is made good in the
+// end: (x - m) c = d + delta.  Where m c is beyond fp32 (CAREFUL: rows of the lowest value, or of huge ones) d is (x - m) c.  T is kept for ENTROPY.
+constexpr float kFarOff = 1e38f;  // |m c| from here on is not for the quick form
+template <bool CAREFUL, bool ENTROPY>
+struct Way {
+    Sums a;
+    float q;
+    __device__ __forceinline__ void begin() { a = no_sums(), q = kLowest; }
+    __device__ __forceinline__ void absorb(const float (&x)[kRowUnit], float top, float c)
+    {
+        const float m = fmaxf(a.m, top);
+        if constexpr (CAREFUL) {
+            move_to(a, m, c);
+        } else {
+            const float to = fmaxf(m * c, kLowest), shift = fminf(to - q, kFar), f = exp2_of(-shift);
+            if constexpr (ENTROPY) a.T = f * fmaf(-shift, a.S, a.T);
+            a.S *= f;
+            a.m = m;
+            q = to;
+        }
 #pragma unroll
-    for (int j = 0; j < kRowUnit; ++j) {
-        const float d = (x[j] - a.m) * c, e = exp2_of(d);
-        a.S += e;
-        a.T = fmaf(e, fmaxf(d, -kFar), a.T);
+        for (int j = 0; j < kRowUnit; ++j) {
+            const float d = CAREFUL ? (x[j] - a.m) * c : fmaf(x[j], c, -q), e = exp2_of(d);
+            a.S += e;
+            if constexpr (ENTROPY) a.T = fmaf(e, fmaxf(d, -kFar), a.T);
+        }
     }
-}
+    __device__ __forceinline__ Sums end(float c)
+    {
+        if constexpr (!CAREFUL) {
+            const float delta = fabsf(q) < kFarOff ? fmaf(-a.m, c, q) : 0.f, f = exp2_of(delta);
+            if constexpr (ENTROPY) a.T = f * fmaf(delta, a.S, a.T);
+            a.S *= f;
+        }
+        return a;
+    }
+};
 
+// (the same bits whichever comes first, so that all lanes that join each other's have the same: no product may be taken into the addition of one side)
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
 {
+#pragma clang fp contract(off)
     const float m = fmaxf(a.m, b.m);
     move_to(a, m, c);
     move_to(b, m, c);
@@ -239,23 +269,28 @@ struct Entries {  // of the teacher, in LDS
 
 constexpr auto kMax = [](float a, float b) { return fmaxf(a, b); };
 
-template <int T, typename F>
-__device__ __forceinline__ float over_workgroup(float x, float* room, F&& f)  // (two barriers)
+// Of several entries of a column the first one has their sum.  Few entries are seen to by the wavefront that takes them, while the others go through the row; more
+// by all threads in the end.
+constexpr int kFewEntries = 2 * kWave;
+__device__ __forceinline__ void sum_of_column(const ClassCall& C, const Entries& E, int i, float& sum, bool& mine)
 {
-    x = over_lanes<kWave>(x, f);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
-    __syncthreads();
-    return over_lanes<T / kWave>(room[threadIdx.x % (T / kWave)], f);
+    sum = 0.f;
+    mine = i < C.k;
+    const int col = mine ? E.col[i] : -1;
+    for (int j = 0; j < C.k; ++j)
+        if (E.col[j] == col) {
+            mine &= j >= i;
+            sum += E.q[j];
+        }
 }
 
-// The teacher's entries of a row, their q and the student's x there.  An entry whose column lies outside the row is none.
-template <int VT, int T>
-__device__ Asked take_entries(const ClassCall& C, int64_t row, Entries& E, float* room)
+// The teacher's entries of a row by one wavefront: their q and the student's x there.  An entry whose column lies outside the row is none.
+template <int VT>
+__device__ Asked take_entries(const ClassCall& C, int64_t row, int lane, Entries& E)
 {
     const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
     float top = kLowest, ref = kLowest;
-    for (int i = threadIdx.x; i < C.k; i += T) {
+    for (int i = lane; i < C.k; i += kWave) {
         const int64_t col = column_of(C, row * C.k + i);
         const bool there = col >= 0 && col < C.V;
         E.col[i] = there ? (int32_t)col : -1;
@@ -264,21 +299,34 @@ __device__ Asked take_entries(const ClassCall& C, int64_t row, Entries& E, float
         top = fmaxf(top, E.q[i]);
         ref = fmaxf(ref, E.x[i]);
     }
-    top = over_workgroup<T>(top, room, kMax);
-    ref = over_workgroup<T>(ref, room, kMax);
+    top = over_lanes<kWave>(top, kMax);
+    ref = over_lanes<kWave>(ref, kMax);
     const float c = C.scale * kLog2e;
     float sum = 0.f;
-    for (int i = threadIdx.x; i < C.k; i += T) sum += exp2_of((E.q[i] - top) * c);
-    sum = over_workgroup<T>(sum, room, kAdd);
+    for (int i = lane; i < C.k; i += kWave) sum += exp2_of((E.q[i] - top) * c);
+    sum = over_lanes<kWave>(sum, kAdd);
     const float ln = logf(sum), inverse = 1.f / sum;
     float loss = 0.f;
-    for (int i = threadIdx.x; i < C.k; i += T) {
+    for (int i = lane; i < C.k; i += kWave) {
         const float d = (E.q[i] - top) * c, q = sum == 0.f ? 0.f : exp2_of(d) * inverse;
         if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - (E.x[i] - ref) * C.scale);
         E.q[i] = q;
     }
-    loss = over_workgroup<T>(loss, room, kAdd);
-    return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
+    if (C.dlogits && C.k <= kFewEntries) {
+        wave_fence();
+        float all[kFewEntries / kWave];
+        bool mine[kFewEntries / kWave];
+#pragma unroll
+        for (int r = 0; r < kFewEntries / kWave; ++r) sum_of_column(C, E, lane + r * kWave, all[r], mine[r]);
+        wave_fence();
+#pragma unroll
+        for (int r = 0; r < kFewEntries / kWave; ++r)
+            if (const int i = lane + r * kWave; i < C.k) {
+                E.q[i] = all[r];
+                if (!mine[r]) E.col[i] = -1;
+            }
+    }
+    return {0.f, over_lanes<kWave>(loss, kAdd), ref, sum == 0.f ? 0.f : sum * inverse};
 }
 
 template <int VT>
@@ -337,100 +385,168 @@ __device__ __forceinline__ Slope row_slope(const ClassCall& C, int64_t row, cons
     return {(-g + u * (f.ln - f.entropy)) * inverse, -u * kLn2 * inverse, g, y};
 }
 
+// Columns from `first` on up to the next line of 128 bytes in memory (fewer: up to `last`)
+template <int VT>
+__device__ __forceinline__ int line_start(const value_store_t<VT>* row, int first, int last)
+{
+    constexpr int kSize = sizeof(value_store_t<VT>);
+    const int past = (int)(reinterpret_cast<uintptr_t>(row + first) & 127);
+    return min(first + (past ? (128 - past) / kSize : 0), last);
+}
+
+// Columns [first, last) of a row by a workgroup, `whole` being where its lines start (line_start): those before it and those behind the last whole step (32 bytes a
+// thread, kStep units) go to part(unit, column, valid columns), then the steps to step(units, first one's column), each while the next one is under way.
+template <int VT> constexpr int kStep = VT == MAXK_VALUE_F32 ? 1 : 2;
+template <int VT, int T, typename F, typename G>
+__device__ __forceinline__ void walk(const value_store_t<VT>* x, int first, int whole, int last, const value_store_t<VT>* end, F&& step, G&& part)
+{
+    constexpr int K = kStep<VT>, kRun = T * kRowUnit, kWhole = K * kRun;
+    const int at = threadIdx.x * kRowUnit, rest = whole + (last - whole) / kWhole * kWhole;
+    const RawUnit<VT> head = fetch_row_unit<VT>(x + first + at, whole - first - at, end);
+    RawUnit<VT> tail[K], raw[K] = {};
+#pragma unroll
+    for (int i = 0; i < K; ++i) tail[i] = fetch_row_unit<VT>(x + rest + i * kRun + at, last - rest - i * kRun - at, end);
+    if (whole < rest) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) raw[i] = whole_unit<VT>(x + whole + i * kRun + at);
+    }
+    if (first < whole) part(head, first + at, whole - first - at);
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (rest + i * kRun < last) part(tail[i], rest + i * kRun + at, last - rest - i * kRun - at);
+    if (whole == rest) return;
+    int base = whole;
+    for (; base + kWhole < rest; base += kWhole) {
+        RawUnit<VT> next[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) next[i] = whole_unit<VT>(x + base + kWhole + i * kRun + at);
+        step(raw, base + at);
+#pragma unroll
+        for (int i = 0; i < K; ++i) raw[i] = next[i];
+    }
+    step(raw, base + at);
+}
+
 // Columns [first, last) of a row by a workgroup: their sums, and the likeliest of them in every wavefront
-template <int VT, int T, bool TOP>
+template <int VT, int T, bool CAREFUL, bool ENTROPY, bool TOP>
 __device__ __forceinline__ Sums sum_columns(const ClassCall& C, int64_t row, int first, int last, Likeliest& best)
 {
     using S = value_store_t<VT>;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
     const float c = C.scale * kLog2e;
-    Sums sums = no_sums();
-    int base = first;
+    Way<CAREFUL, ENTROPY> sums;
+    sums.begin();
     bool begun = false;
-    for (; base + 2 * T * kRowUnit <= last; base += 2 * T * kRowUnit) {  // two units under way
-        const int col = base + threadIdx.x * kRowUnit, next = col + T * kRowUnit;
-        float v[2][kRowUnit];
-        load_whole_unit<VT>(x + col, v[0]);
-        load_whole_unit<VT>(x + next, v[1]);
-        const float top = largest(v[0]), other = largest(v[1]);
-        absorb(sums, v[0], top, c);
-        absorb(sums, v[1], other, c);
-        if constexpr (TOP) {
-            if (!begun) best.expect(fmaxf(top, other), true);
-            begun = true;
-            best.offer(v[0], top, col, kRowUnit);
-            best.offer(v[1], other, next, kRowUnit);
-        }
-    }
-    for (; base < last; base += T * kRowUnit) {
-        const int col = base + threadIdx.x * kRowUnit;
+    const auto part = [&](const RawUnit<VT>& raw, int col, int valid) {
         float v[kRowUnit];
-        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
+        unit_values<VT>(raw, valid, -__builtin_inff(), v);
         const float top = largest(v);
-        absorb(sums, v, top, c);
+        sums.absorb(v, top, c);
         if constexpr (TOP) {
-            if (!begun) best.expect(top, col < last);
+            if (!begun) best.expect(top, valid > 0);
             begun = true;
-            best.offer(v, top, col, last - col);
+            best.offer(v, top, col, valid);
         }
+    };
+    walk<VT, T>(
+        x, first, first, last, end,  // (wherever it lies: the sums' bits do not depend on it)
+        [&](const RawUnit<VT>(&raw)[kStep<VT>], int col) {
+            float v[kStep<VT>][kRowUnit], top[kStep<VT>], most;
+#pragma unroll
+            for (int i = 0; i < kStep<VT>; ++i) {
+                unit_values<VT>(raw[i], kRowUnit, 0.f, v[i]);
+                top[i] = largest(v[i]);
+                most = i ? fmaxf(most, top[i]) : top[i];
+            }
+#pragma unroll
+            for (int i = 0; i < kStep<VT>; ++i) sums.absorb(v[i], top[i], c);
+            if constexpr (TOP) {
+                if (!begun) best.expect(most, true);
+                begun = true;
+#pragma unroll
+                for (int i = 0; i < kStep<VT>; ++i) best.offer(v[i], top[i], col + i * T * kRowUnit, kRowUnit);
+            }
+        },
+        part);
+    return sums.end(c);
+}
+
+__device__ __forceinline__ bool far_off(const Sums& s, float c) { return !(fabsf(s.m * c) < kFarOff); }
+
+// The workgroup's sums of these columns (`room` is free behind the next barrier); what other wavefronts left in LDS before is there
+template <int VT, int T, bool ENTROPY, bool TOP>
+__device__ __forceinline__ Sums sum_row(const ClassCall& C, int64_t row, int first, int last, Likeliest& best, Sums* room)
+{
+    const float c = C.scale * kLog2e;
+    Sums s = join_workgroup<T>(sum_columns<VT, T, false, ENTROPY, TOP>(C, row, first, last, best), c, room);
+    if (far_off(s, c)) {
+        s = sum_columns<VT, T, true, ENTROPY, false>(C, row, first, last, best);
+        __syncthreads();
+        s = join_workgroup<T>(s, c, room);
     }
-    return sums;
+    return s;
 }
 
 // Their gradient; distillation's entries in these columns follow
-template <int VT, int T, bool DISTILL>
-__device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
+template <int VT, int T, bool CAREFUL, bool DISTILL>
+__device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
 {
     using S = value_store_t<VT>;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
     S* dx = (S*)C.dlogits + row * C.V;
-    const float c = C.scale * kLog2e;
-    const auto slope = [&](float v) {
-        const float d = fmaxf((v - s.m) * c, -kFar);
-        return exp2_of(d) * (DISTILL ? k.A : fmaf(k.B, d, k.A));
+    // (the quick form of d as in Way: its rest goes into A and B)
+    const float c = C.scale * kLog2e, q = s.m * c, delta = CAREFUL ? 0.f : fmaf(-s.m, c, q), f = exp2_of(delta), A = f * fmaf(k.B, delta, k.A), B = f * k.B;
+    const auto slope = [&](float v, float g) {  // (one rounding, whichever way a column comes here: bits do not depend on where the row starts)
+        const float d = CAREFUL ? (v - s.m) * c : fmaf(v, c, -q);
+        return fmaf(exp2_of(d), DISTILL ? A : fmaf(B, fmaxf(d, -kFar), A), g);
     };
     const auto unit = [&](float (&v)[kRowUnit], int col) {
-#pragma unroll
-        for (int j = 0; j < kRowUnit; ++j) v[j] = slope(v[j]);
         if (!DISTILL && (uint64_t)(k.y - col) < kRowUnit) {
 #pragma unroll
-            for (int j = 0; j < kRowUnit; ++j) v[j] += j == (int)(k.y - col) ? k.g : 0.f;
+            for (int j = 0; j < kRowUnit; ++j) v[j] = slope(v[j], j == (int)(k.y - col) ? k.g : 0.f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j) v[j] = slope(v[j], 0.f);
         }
     };
-    int base = first;
-    for (; base + 2 * T * kRowUnit <= last; base += 2 * T * kRowUnit) {
-        const int col = base + threadIdx.x * kRowUnit, next = col + T * kRowUnit;
-        float v[2][kRowUnit];
-        load_whole_unit<VT>(x + col, v[0]);
-        load_whole_unit<VT>(x + next, v[1]);
-        unit(v[0], col);
-        store_whole_unit<VT>(dx + col, v[0]);
-        unit(v[1], next);
-        store_whole_unit<VT>(dx + next, v[1]);
-    }
-    for (; base < last; base += T * kRowUnit) {
-        const int col = base + threadIdx.x * kRowUnit;
-        if (col >= last) break;
-        float v[kRowUnit];
-        load_row_unit<VT>(x + col, last - col, end, -__builtin_inff(), v);
-        unit(v, col);
-        store_row_unit<VT>(dx + col, last - col, v);
-    }
+    const bool once = past_l2(C.N * C.V * (int64_t)sizeof(S));
+    walk<VT, T>(
+        x, first, line_start<VT>(dx, first, last), last, end,
+        [&](const RawUnit<VT>(&raw)[kStep<VT>], int col) {
+#pragma unroll
+            for (int i = 0; i < kStep<VT>; ++i, col += T * kRowUnit) {
+                float v[kRowUnit];
+                unit_values<VT>(raw[i], kRowUnit, 0.f, v);
+                unit(v, col);
+                if (once) store_unit_once<VT>(dx + col, v);
+                else store_whole_unit<VT>(dx + col, v);
+            }
+        },
+        [&](const RawUnit<VT>& raw, int col, int valid) {
+            if (valid < 1) return;
+            float v[kRowUnit];
+            unit_values<VT>(raw, valid, 0.f, v);
+            unit(v, col);
+            store_row_unit<VT>(dx + col, valid, v);
+        });
     if constexpr (DISTILL) {
         __syncthreads();  // what is stored above at their columns is stored again
         for (int i = threadIdx.x; i < C.k; i += T) {
             const int col = E->col[i];
             if (col < first || col >= last) continue;
-            float q = 0.f;
-            bool mine = true;  // of several entries of a column the first one has the sum
-            for (int j = 0; j < C.k; ++j)
-                if (E->col[j] == col) {
-                    mine &= j >= i;
-                    q += E->q[j];
-                }
-            if (mine) dx[col] = round_value<VT>(fmaf(-k.g, q, slope(E->x[i])));
+            float sum = E->q[i];
+            bool mine = true;
+            if (C.k > kFewEntries) sum_of_column(C, *E, i, sum, mine);
+            if (mine) dx[col] = round_value<VT>(slope(E->x[i], -k.g * sum));
         }
     }
+}
+
+template <int VT, int T, bool DISTILL>
+__device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
+{
+    if (far_off(s, C.scale * kLog2e)) store_columns<VT, T, true, DISTILL>(C, row, first, last, s, k, E);
+    else store_columns<VT, T, false, DISTILL>(C, row, first, last, s, k, E);
 }
 
 // ---- a row in the registers of L lanes, U units of 8 columns each ----
@@ -616,10 +732,10 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
 // ---- a workgroup a row ----
 
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
-__global__ void __launch_bounds__(T) class_rows_kernel(ClassCall C)
+__global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
 {
-    __shared__ Sums sums_room[T / kWave];
-    __shared__ float room[T / kWave];
+    __shared__ Sums room[T / kWave];
+    __shared__ Asked asked_room;
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
     const int64_t row = blockIdx.x;
@@ -627,10 +743,16 @@ __global__ void __launch_bounds__(T) class_rows_kernel(ClassCall C)
     Likeliest best;
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
     Asked asked;
-    if constexpr (DISTILL) asked = take_entries<VT, T>(C, row, entries, room);
-    else asked = given_class<VT>(C, row);
-    Sums s = sum_columns<VT, T, TOP>(C, row, 0, C.V, best);
-    s = join_workgroup<T>(s, C.scale * kLog2e, sums_room);
+    if constexpr (DISTILL) {
+        if (wave == 0) {
+            asked = take_entries<VT>(C, row, lane, entries);
+            if (lane == 0) asked_room = asked;
+        }
+    } else {
+        asked = given_class<VT>(C, row);
+    }
+    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, 0, C.V, best, room);
+    if constexpr (DISTILL) asked = asked_room;
     const Found f = row_results(C, row, s, asked);
     if constexpr (TOP) {
         best.end();
@@ -658,8 +780,7 @@ template <int VT, bool DISTILL, bool TOP>
 __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Parts P)
 {
     constexpr int T = kThreads;
-    __shared__ Sums sums_room[T / kWave];
-    __shared__ float room[T / kWave];
+    __shared__ Sums room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
     const int64_t row = blockIdx.x / P.segments;
@@ -667,14 +788,13 @@ __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Part
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     Likeliest best;
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
-    if (segment == 0) {
+    if (segment == 0 && wave == 0) {
         Asked asked;
-        if constexpr (DISTILL) asked = take_entries<VT, T>(C, row, entries, room);
+        if constexpr (DISTILL) asked = take_entries<VT>(C, row, lane, entries);
         else asked = given_class<VT>(C, row);
-        if (threadIdx.x == 0) P.asked[row] = asked;
+        if (lane == 0) P.asked[row] = asked;
     }
-    Sums s = sum_columns<VT, T, TOP>(C, row, first, last, best);
-    s = join_workgroup<T>(s, C.scale * kLog2e, sums_room);
+    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, first, last, best, room);
     if (threadIdx.x == 0) P.sums[blockIdx.x] = s;
     if constexpr (TOP) {
         best.end();
@@ -716,14 +836,15 @@ template <int VT, bool DISTILL>
 __global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, Parts P)
 {
     constexpr int T = kThreads;
-    __shared__ Sums sums_room[T / kWave];
-    __shared__ float room[T / kWave];
+    __shared__ Sums room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     const int64_t row = blockIdx.x / P.segments;
     const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
-    const Sums s = join_segments<T>(C, P, row, sums_room);
+    // (x of other segments may have been overwritten: of the entries only those of this one are used)
+    if constexpr (DISTILL)
+        if (threadIdx.x < kWave) take_entries<VT>(C, row, threadIdx.x, entries);
+    const Sums s = join_segments<T>(C, P, row, room);
     const Asked asked = P.asked[row];
-    if constexpr (DISTILL) take_entries<VT, T>(C, row, entries, room);  // (x of other segments may have been overwritten: only those of this one are used)
     const Found f = row_results(C, row, s, asked);
     if (segment == 0 && threadIdx.x == 0) store_results(C, row, f);
     const Slope k = row_slope(C, row, s, asked, f);
@@ -731,8 +852,13 @@ __global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, P
     else store_gradient<VT, T, false>(C, row, first, last, s, k, nullptr);
 }
 
-// Rows of so many columns take workgroups of 1024 threads
-constexpr int kWideRow = 16384;
+// Threads of a workgroup that has a row.  The gradient reads its rows again: those that all CUs work on at a time have to stay in the Infinity Cache.
+template <int VT>
+int threads_of(int V)
+{
+    const double of_256 = 256.0 * 8 * V * sizeof(value_store_t<VT>), most = 128.0 * (1 << 20);
+    return of_256 <= most ? 256 : of_256 <= 2 * most ? 512 : 1024;
+}
 
 // Segments of a row
 struct Cut { int segments, width; };
@@ -777,7 +903,14 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     if (units <= 128) return run_teams<VT, 64, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
-    if (cut.segments == 1) return C.V >= kWideRow ? run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s) : run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);
+    if (cut.segments == 1) {
+        const int T = GRAD ? threads_of<VT>(C.V) : kThreads;
+        if constexpr (GRAD) {
+            if (T == 1024) return run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s);
+            if (T == 512) return run_rows<VT, 512, DISTILL, GRAD, TOP>(C, s);
+        }
+        return run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);
+    }
     char* at = (char*)workspace;
     Parts P = {cut.segments, cut.width, (Sums*)at, nullptr, nullptr};
     at += up16(C.N * cut.segments * (int64_t)sizeof(Sums));

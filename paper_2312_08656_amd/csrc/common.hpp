@@ -17,7 +17,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Streams that a kernel reads or writes once pass by the L2's replacement order, so that the records it gathers stay.
 // Forward output below the size of the eight L2s together is better left there: its way out would add to the end of a short kernel
 // (forward, 2.1 M entries on 4 k nodes 28.1 us plain / 29.0; 1.2 M on 40 k 40.0 / 40.9; 169 k nodes, 173 MB of Y 99.9 / 98.9).
-inline bool past_l2(int64_t bytes) { return bytes > (32 << 20); }
+__host__ __device__ inline bool past_l2(int64_t bytes) { return bytes > (32 << 20); }
 
 // The products of expand/reduce, which one kernel writes and the next one reads.  They pass by L2 where they do not fit the
 // Infinity Cache (256 MiB) with the rest of the pass: entries, dY, columns, result, and H, Y and dH around the call.  Within it the

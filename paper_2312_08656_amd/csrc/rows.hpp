@@ -70,6 +70,20 @@ __device__ __forceinline__ void store_whole_unit(value_store_t<VT>* p, const flo
     __builtin_memcpy(p, v, sizeof(v));
 }
 
+// the same past the caches, to an address of whole 16 bytes
+template <int VT>
+__device__ __forceinline__ void store_unit_once(value_store_t<VT>* p, const float (&x)[kRowUnit])
+{
+    typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+    value_store_t<VT> v[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) v[j] = round_value<VT>(x[j]);
+    u32x4v w[VT == MAXK_VALUE_F32 ? 2 : 1];
+    __builtin_memcpy(&w, v, sizeof(v));
+    __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4v*>(p));
+    if constexpr (VT == MAXK_VALUE_F32) __builtin_nontemporal_store(w[1], reinterpret_cast<u32x4v*>(p + 4));
+}
+
 // Unit at p, of which `valid` columns (less than 1: none) belong to the row.  What lies behind a row is read where it belongs to the matrix, which ends at
 // `end`.  (Values are taken out apart from it: a lane's units are under way together.)
 template <int VT>
