@@ -564,69 +564,131 @@ __device__ __forceinline__ uint64_t unpaired(double key)
     return high < 0x3FF00000u ? 0 : (uint64_t)(high << 12 | low >> 20) << 32 | (0xFFFFFFFFu - (0xFFFFFu - (low & 0xFFFFFu)));
 }
 
-// Entries of the teacher: the loss's part, and (GRAD) the sums of q at every column to `spread`, LDS for the columns of the row
+// Entries of the teacher by the lanes of a row: the loss's part, and (GRAD) the sums of q at every column to `spread`, LDS for the columns of the row.
 template <int VT, int L, int U, bool GRAD>
-__device__ __forceinline__ Asked team_entries(const ClassCall& C, int64_t row, int lane, float* spread)
-{
-    const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
-    const float c = C.scale * kLog2e;
-    const auto column = [&](int i) {
-        const int64_t col = column_of(C, row * C.k + i);
+struct TeamEntries {
+    const ClassCall& C;
+    const value_store_t<VT>* x;
+    int64_t at;
+    int lane, first;   // column of the lane's own entry, which it has where there are no more than lanes
+    float own;
+    float* spread;
+
+    __device__ __forceinline__ int column(int i) const
+    {
+        const int64_t col = column_of(C, at + i);
         return col >= 0 && col < C.V ? (int)col : -1;
-    };
-    const auto value = [&](int i, int col) { return col >= 0 ? teacher_value(C, row * C.k + i) : -__builtin_inff(); };
-    float top = kLowest, ref = kLowest;
-    for (int i = lane; i < C.k; i += L) {
-        const int col = column(i);
-        top = fmaxf(top, value(i, col));
-        if (col >= 0) ref = fmaxf(ref, widen_value<VT>(x[col]));
     }
-    top = over_lanes<L>(top, kMax);
-    ref = over_lanes<L>(ref, kMax);
-    float sum = 0.f;
-    for (int i = lane; i < C.k; i += L) sum += exp2_of((value(i, column(i)) - top) * c);
-    sum = over_lanes<L>(sum, kAdd);
-    const float ln = logf(sum), inverse = 1.f / sum;
-    const auto weight = [&](float d) { return sum == 0.f ? 0.f : exp2_of(d) * inverse; };
-    if constexpr (GRAD) {
+    __device__ __forceinline__ float value(int i, int col) const { return col >= 0 ? teacher_value(C, at + i) : -__builtin_inff(); }
+    __device__ __forceinline__ float logit(int col) const { return col >= 0 ? widen_value<VT>(x[col]) : -__builtin_inff(); }
+
+    __device__ __forceinline__ TeamEntries(const ClassCall& C_, int64_t row, int lane_, float* spread_)
+        : C(C_), x((const value_store_t<VT>*)C_.logits + row * C_.V), at(row * C_.k), lane(lane_), spread(spread_)
+    {
+        if (C.k > L) return;
+        first = lane < C.k ? column(lane) : -1;
+        own = value(lane, first);
+    }
+
+    // columns without an entry have 0; those of one have the entry's number + 1 (of several: of one of them).  Whether there are several
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < kRowUnit; j += 4) *reinterpret_cast<float4*>(spread + (lane + u * L) * kRowUnit + j) = make_float4(0.f, 0.f, 0.f, 0.f);
         wave_fence();
-        for (int i = lane; i < C.k; i += L)
-            if (const int col = column(i); col >= 0) spread[col] = __int_as_float(i + 1);  // (whose entry is to write there: one of them where there are several)
-        wave_fence();
     }
-    float loss = 0.f;
-    bool several = false;
-    for (int i = lane; i < C.k; i += L) {
-        const int col = column(i);
-        const float d = (value(i, col) - top) * c, q = weight(d);
-        if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - ((col >= 0 ? widen_value<VT>(x[col]) : -__builtin_inff()) - ref) * C.scale);
-        if constexpr (GRAD) several |= col >= 0 && __float_as_int(spread[col]) != i + 1;
+    __device__ __forceinline__ bool others(int i, int col) const { return col >= 0 && __float_as_int(spread[col]) != i + 1; }
+    __device__ __forceinline__ bool any(bool b) const { return over_lanes<L>((uint32_t)b, [](uint32_t p, uint32_t q) { return p | q; }) != 0; }
+
+    __device__ __forceinline__ Asked take()
+    {
+        const float c = C.scale * kLog2e;
+        return C.k <= L ? take_one(c) : take_more(c);
     }
-    if constexpr (GRAD) {
-        // (all lanes' marks are read before the first sum is written)
-        several = over_lanes<L>((uint32_t)several, [](uint32_t a, uint32_t b) { return a | b; });
-        wave_fence();
+
+    __device__ __forceinline__ Asked take_one(float c)
+    {
+        const float xs = logit(first), top = over_lanes<L>(fmaxf(own, kLowest), kMax), ref = over_lanes<L>(fmaxf(xs, kLowest), kMax);
+        const float d = (own - top) * c, e = exp2_of(d), sum = over_lanes<L>(e, kAdd), ln = logf(sum), inverse = 1.f / sum;
+        float q = sum == 0.f ? 0.f : e * inverse;
+        const float loss = over_lanes<L>(q != 0.f ? q * (fmaf(kLn2, d, -ln) - (xs - ref) * C.scale) : 0.f, kAdd);
+        if constexpr (GRAD) {
+            clear();
+            if (first >= 0) spread[first] = __int_as_float(lane + 1);
+            wave_fence();
+            const bool other = others(lane, first);
+            if (any(other)) {  // sums in the entries' order
+                float all = 0.f;
+                for (int j = 0; j < C.k; ++j) {
+                    const int col = __shfl(first, j, L);
+                    const float p = __shfl(q, j, L);
+                    all += col == first ? p : 0.f;
+                }
+                q = all;
+            }
+            wave_fence();
+            if (first >= 0 && !other) spread[first] = q;
+            wave_fence();
+        }
+        return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
+    }
+
+    __device__ Asked take_more(float c)
+    {
+        float top = kLowest, ref = kLowest;
         for (int i = lane; i < C.k; i += L) {
             const int col = column(i);
-            if (col < 0) continue;
-            float q = 0.f;
-            if (several) {  // sums in the entries' order
-                if (__float_as_int(spread[col]) != i + 1) continue;
-                for (int j = 0; j < C.k; ++j)
-                    if (column(j) == col) q += weight((value(j, col) - top) * c);
-            } else {
-                q = weight((value(i, col) - top) * c);
-            }
-            spread[col] = q;
+            top = fmaxf(top, value(i, col));
+            ref = fmaxf(ref, logit(col));
         }
-        wave_fence();
+        top = over_lanes<L>(top, kMax);
+        ref = over_lanes<L>(ref, kMax);
+        float sum = 0.f;
+        for (int i = lane; i < C.k; i += L) sum += exp2_of((value(i, column(i)) - top) * c);
+        sum = over_lanes<L>(sum, kAdd);
+        const float ln = logf(sum), inverse = 1.f / sum;
+        const auto weight = [&](float d) { return sum == 0.f ? 0.f : exp2_of(d) * inverse; };
+        if constexpr (GRAD) {
+            clear();
+            for (int i = lane; i < C.k; i += L)
+                if (const int col = column(i); col >= 0) spread[col] = __int_as_float(i + 1);
+            wave_fence();
+        }
+        float loss = 0.f;
+        bool several = false;
+        for (int i = lane; i < C.k; i += L) {
+            const int col = column(i);
+            const float d = (value(i, col) - top) * c, q = weight(d);
+            if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - (logit(col) - ref) * C.scale);
+            if constexpr (GRAD) several |= others(i, col);
+        }
+        if constexpr (GRAD) {
+            several = any(several);  // (all marks are read before the first sum is written)
+            wave_fence();
+            for (int i = lane; i < C.k; i += L) {
+                const int col = column(i);
+                if (col < 0) continue;
+                float q = 0.f;
+                if (several) {  // sums in the entries' order.  (an entry that finds a sum where its mark was writes the same sum)
+                    if (others(i, col)) continue;
+                    for (int j = 0; j < C.k; ++j)
+                        if (column(j) == col) q += weight((value(j, col) - top) * c);
+                } else {
+                    q = weight((value(i, col) - top) * c);
+                }
+                spread[col] = q;
+            }
+            wave_fence();
+        }
+        return {0.f, over_lanes<L>(loss, kAdd), ref, sum == 0.f ? 0.f : sum * inverse};
     }
-    return {0.f, over_lanes<L>(loss, kAdd), ref, sum == 0.f ? 0.f : sum * inverse};
-}
+};
+
+struct Nothing {
+    __device__ __forceinline__ Nothing(const ClassCall&, int64_t, int, float*) {}
+};
 
 template <int VT, int L, int U, bool DISTILL, bool GRAD, bool TOP>
 __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
@@ -648,8 +710,8 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     }
     float* mine = spread + (DISTILL && GRAD ? team * L * U * kRowUnit : 0);
     Asked asked;
-    if constexpr (DISTILL) asked = team_entries<VT, L, U, GRAD>(C, row, lane, mine);
-    else asked = given_class<VT>(C, row);
+    std::conditional_t<DISTILL, TeamEntries<VT, L, U, GRAD>, Nothing> entries(C, row, lane, mine);
+    if constexpr (!DISTILL) asked = given_class<VT>(C, row);
     float v[U][kRowUnit];
 #pragma unroll
     for (int u = 0; u < U; ++u) unit_values<VT>(raw[u], C.V - (lane + u * L) * kRowUnit, -__builtin_inff(), v[u]);
@@ -670,6 +732,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         }
     s.S = over_lanes<L>(s.S, kAdd);
     if constexpr (!DISTILL) s.T = over_lanes<L>(s.T, kAdd);
+    if constexpr (DISTILL) asked = entries.take();
     const Found f = row_results(C, row, s, asked);
     if (lane == 0) store_results(C, row, f);
     if constexpr (TOP && L == kWave) {
