@@ -130,49 +130,44 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
 {
     return (uint64_t)(uint32_t)__shfl((int)(k >> 32), lane) << 32 | (uint32_t)__shfl((int)(uint32_t)k, lane);
 }
+__device__ __forceinline__ uint64_t key_of_lane(uint64_t k, int lane)  // (the same lane for all)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
 __device__ __forceinline__ uint64_t greater_key(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // of lane ^ STEP
 template <int STEP>
 __device__ __forceinline__ uint32_t across(uint32_t x)
 {
-    if constexpr (STEP == 4) x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true), x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x1B, 0xF, 0xF, true);  // row_half_mirror, quad_perm [3,2,1,0]
-    else if constexpr (STEP == 8) x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true);  // row_ror:8
+    if constexpr (STEP == 4) x = dpp<0x1B>(dpp<0x141>(x));  // row_half_mirror, quad_perm [3,2,1,0]
+    else if constexpr (STEP == 8) x = dpp<0x128>(x);        // row_ror:8
     else x = xor_lane(x, std::integral_constant<int, STEP>{});
     return x;
 }
 template <int STEP>
-__device__ __forceinline__ uint64_t exchange(uint64_t k, int lane, bool falling)
+__device__ __forceinline__ uint64_t exchange(uint64_t k, int lane)
 {
     const uint64_t o = (uint64_t)across<STEP>((uint32_t)(k >> 32)) << 32 | across<STEP>((uint32_t)k);
-    return (((lane & STEP) == 0) == falling) == (k > o) ? k : o;
+    return ((lane & STEP) == 0) == (k > o) ? k : o;
 }
-// runs of 2 STEP lanes whose halves are in opposite orders into order, falling where (lane & RUN) is 0
-template <int STEP, int RUN>
+// runs of 2 STEP lanes whose halves are in opposite orders into falling order
+template <int STEP>
 __device__ __forceinline__ uint64_t settle(uint64_t k, int lane)
 {
-    k = exchange<STEP>(k, lane, (lane & RUN) == 0);
-    if constexpr (STEP > 1) k = settle<STEP / 2, RUN>(k, lane);
+    k = exchange<STEP>(k, lane);
+    if constexpr (STEP > 1) k = settle<STEP / 2>(k, lane);
     return k;
-}
-// keys of the 64 lanes in falling order (equal ones only where both are 0)
-__device__ __forceinline__ uint64_t sort_keys(uint64_t k, int lane)
-{
-    k = settle<1, 2>(k, lane);
-    k = settle<2, 4>(k, lane);
-    k = settle<4, 8>(k, lane);
-    k = settle<8, 16>(k, lane);
-    k = settle<16, 32>(k, lane);
-    return settle<32, 64>(k, lane);
 }
 // the 64 greatest of two sets in falling order, in falling order
 __device__ __forceinline__ uint64_t merge_keys(uint64_t a, uint64_t b, int lane)
 {
-    return settle<32, 64>(greater_key(a, lane_key(b, 63 - lane)), lane);
+    return settle<32>(greater_key(a, lane_key(b, 63 - lane)), lane);
 }
+constexpr int kWaiting = kWave * (kRowUnit + 1);  // keys of a wavefront that wait to be sorted in: a unit of every lane on top of less than a wavefront's
 // of the wavefronts of a workgroup, for the first of them (keys: 64 of each, written)
-template <int T>
-__device__ __forceinline__ uint64_t merge_waves(uint64_t mine, uint64_t (*keys)[2 * kWave], int lane, int wave)
+template <int T, int ROOM>
+__device__ __forceinline__ uint64_t merge_waves(uint64_t mine, uint64_t (&keys)[T / kWave][ROOM], int lane, int wave)
 {
     for (int step = 1; step < T / kWave; step *= 2) {
         keys[wave][lane] = mine;
@@ -187,8 +182,9 @@ __device__ __forceinline__ uint64_t merge_waves(uint64_t mine, uint64_t (*keys)[
 struct Likeliest {
     uint64_t mine, least;   // least: of a key that is still wanted (it is greater)
     float least_value;
-    uint64_t* wait;         // 128 keys
+    uint64_t* wait;         // kWaiting keys
     int waiting, k, lane;
+    bool some;              // mine has any
 
     __device__ __forceinline__ void begin(int k_, uint64_t* wait_, int lane_)
     {
@@ -198,44 +194,58 @@ struct Likeliest {
         waiting = 0;
         k = k_;
         lane = lane_;
+        some = false;
     }
     __device__ __forceinline__ void raise(uint64_t key)
     {
         least = key > least ? key : least;
-        least_value = least >> 32 ? key_value((uint32_t)(least >> 32)) : -__builtin_inff();
+        const uint32_t high = (uint32_t)(least >> 32);  // (a bound cut short may lie below -Inf's key)
+        least_value = high > 0x007FFFFFu ? key_value(high) : -__builtin_inff();
     }
+    // Up to 64 of the waiting keys into the order: a key's place is the number of greater ones, which it counts
     __device__ void sort_in()
     {
         wave_fence();
         const int n = min(waiting, kWave), from = waiting - n;
         const uint64_t key = lane < n ? wait[from + lane] : 0;
+        int place = 0;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) place += key_of_lane(key, i) > key;
+        wave_fence();
+        if (lane < n) wait[from + place] = key;
+        wave_fence();
+        const uint64_t sorted = lane < n ? wait[from + lane] : 0;
         waiting = from;
-        mine = merge_keys(mine, sort_keys(key, lane), lane);
-        raise(lane_key(mine, k - 1));
+        mine = some ? merge_keys(mine, sorted, lane) : sorted;
+        some = true;
+        raise(key_of_lane(mine, k - 1));
     }
-    // The k-th greatest of the lanes' largest values is no less than the k-th greatest value of all: a first bound, before anything is offered.
-    // (some: the lane has one)
-    __device__ __forceinline__ void expect(float top, bool some)
+    // The k-th greatest of the lanes' largest values is no less than the k-th greatest value of all: a first bound, its leading 20 bits, before anything is
+    // offered.  (any: the lane has one)
+    __device__ __forceinline__ void expect(float top, bool any)
     {
-        raise((uint64_t)(uint32_t)(lane_key(sort_keys((uint64_t)(some ? value_key(top) : 0u) << 32, lane), k - 1) >> 32) << 32);
+        const uint32_t key = any ? value_key(top) : 0u;
+        uint32_t bound = 0;
+#pragma unroll
+        for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1)
+            if (__popcll(__ballot(key >= (bound | bit))) >= k) bound |= bit;
+        raise((uint64_t)bound << 32);
     }
     // a unit at column `col`: all lanes come here, those without columns with valid < 1
     __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid)
     {
         if (!__any(valid > 0 && top >= least_value)) return;
-#pragma unroll 1
-        for (int j = 0; j < kRowUnit; ++j) {
-            float v = x[0];
 #pragma unroll
-            for (int i = 1; i < kRowUnit; ++i) v = i == j ? x[i] : v;
-            const uint64_t key = key_of(v, (uint32_t)(col + j));
-            const bool wanted = j < valid && key > least;
+        for (int j = 0; j < kRowUnit; ++j) {
+            const bool perhaps = j < valid && x[j] >= least_value;
+            if (!__any(perhaps)) continue;
+            const uint64_t key = key_of(x[j], (uint32_t)(col + j));
+            const bool wanted = perhaps && key > least;
             const uint64_t who = __ballot(wanted);
-            if (!who) continue;
-            if (wanted) wait[waiting + __popcll(who & ((1ull << lane) - 1))] = key;
+            if (wanted) wait[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key;
             waiting += __popcll(who);
-            while (waiting >= kWave) sort_in();
         }
+        while (waiting >= kWave) sort_in();
     }
     __device__ __forceinline__ void end() { while (waiting > 0) sort_in(); }
 };
@@ -397,7 +407,8 @@ __device__ __forceinline__ int line_start(const value_store_t<VT>* row, int firs
 // Columns [first, last) of a row by a workgroup, `whole` being where its lines start (line_start): those before it and those behind the last whole step (32 bytes a
 // thread, kStep units) go to part(unit, column, valid columns), then the steps to step(units, first one's column), each while the next one is under way.
 template <int VT> constexpr int kStep = VT == MAXK_VALUE_F32 ? 1 : 2;
-template <int VT, int T, typename F, typename G>
+// (EDGES_LAST: in the other order, at the price of their registers)
+template <int VT, int T, bool EDGES_LAST, typename F, typename G>
 __device__ __forceinline__ void walk(const value_store_t<VT>* x, int first, int whole, int last, const value_store_t<VT>* end, F&& step, G&& part)
 {
     constexpr int K = kStep<VT>, kRun = T * kRowUnit, kWhole = K * kRun;
@@ -410,11 +421,13 @@ __device__ __forceinline__ void walk(const value_store_t<VT>* x, int first, int 
 #pragma unroll
         for (int i = 0; i < K; ++i) raw[i] = whole_unit<VT>(x + whole + i * kRun + at);
     }
-    if (first < whole) part(head, first + at, whole - first - at);
+    const auto edges = [&] {
+        if (first < whole) part(head, first + at, whole - first - at);
 #pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (rest + i * kRun < last) part(tail[i], rest + i * kRun + at, last - rest - i * kRun - at);
-    if (whole == rest) return;
+        for (int i = 0; i < K; ++i)
+            if (rest + i * kRun < last) part(tail[i], rest + i * kRun + at, last - rest - i * kRun - at);
+    };
+    if (!EDGES_LAST) edges();
     int base = whole;
     for (; base + kWhole < rest; base += kWhole) {
         RawUnit<VT> next[K];
@@ -424,7 +437,8 @@ __device__ __forceinline__ void walk(const value_store_t<VT>* x, int first, int 
 #pragma unroll
         for (int i = 0; i < K; ++i) raw[i] = next[i];
     }
-    step(raw, base + at);
+    if (whole < rest) step(raw, base + at);
+    if (EDGES_LAST) edges();
 }
 
 // Columns [first, last) of a row by a workgroup: their sums, and the likeliest of them in every wavefront
@@ -448,7 +462,7 @@ __device__ __forceinline__ Sums sum_columns(const ClassCall& C, int64_t row, int
             best.offer(v, top, col, valid);
         }
     };
-    walk<VT, T>(
+    walk<VT, T, TOP>(
         x, first, first, last, end,  // (wherever it lies: the sums' bits do not depend on it)
         [&](const RawUnit<VT>(&raw)[kStep<VT>], int col) {
             float v[kStep<VT>][kRowUnit], top[kStep<VT>], most;
@@ -510,7 +524,7 @@ __device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, i
         }
     };
     const bool once = past_l2(C.N * C.V * (int64_t)sizeof(S));
-    walk<VT, T>(
+    walk<VT, T, false>(
         x, first, line_start<VT>(dx, first, last), last, end,
         [&](const RawUnit<VT>(&raw)[kStep<VT>], int col) {
 #pragma unroll
@@ -550,6 +564,20 @@ __device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, 
 }
 
 // ---- a row in the registers of L lanes, U units of 8 columns each ----
+
+// Of keys as doubles, which are none of them NaN: what fmax and fmin would do to NaN first costs as much again
+__device__ __forceinline__ double greater_of(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double lesser_of(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 
 // The k greatest of the L lanes' keys, in turn: a key is a double in [1, 2) whose last 20 bits hold the column, so that the greatest is one operation
 // a step; rows are of at most 2048 columns.  A key that was taken is below 1.
@@ -696,7 +724,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     using S = value_store_t<VT>;
     constexpr int kTeams = kThreads / L;
     __shared__ __attribute__((aligned(16))) float spread[DISTILL && GRAD ? kTeams * L * U * kRowUnit : 1];
-    __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? 2 * kWave : 1];
+    __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? kWaiting : 1];
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t row = (int64_t)blockIdx.x * kTeams + team;
     if (row >= C.N) return;
@@ -755,8 +783,8 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         for (int i = 0; i < C.top_k; ++i) {
             double best = key[0];
 #pragma unroll
-            for (int j = 1; j < kRowUnit; ++j) best = fmax(best, key[j]);
-            best = over_lanes<L>(best, [](double a, double b) { return fmax(a, b); });
+            for (int j = 1; j < kRowUnit; ++j) best = greater_of(best, key[j]);
+            best = over_lanes<L>(best, [](double a, double b) { return greater_of(a, b); });
             const int col = (int)(0xFFFFFu - ((uint32_t)__double2loint(best) & 0xFFFFFu));
 #pragma unroll
             for (int j = 0; j < kRowUnit; ++j)
@@ -792,6 +820,93 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     }
 }
 
+// ---- few classes, few alternatives: a lane a row ----
+
+// Rows of up to 64 columns of which few alternatives are wanted: eight lanes bring a row into LDS, then every lane has one for itself and keeps its K greatest
+// keys in order, two operations a column and key.  (Between lanes a round costs some sixty instructions for each alternative: 2.4 M rows of 47 fp32, 5 of
+// them, 230 us.)  A key of 32 bits has the column in its last 6 and the leading 26 of the value, all that a 16-bit value has.  Of fp32 one more key than alternatives
+// is kept: where two neighbours share their 26 bits, the row is gone through again with keys of 64 bits, twice the time (all of them so: 185 us).
+constexpr int kLaneRowMost = 64, kLaneRowKeys = 8;
+__host__ __device__ constexpr int lane_row_pitch(int V) { return (V + 7) / 8 * 8 + 1; }  // whole units, and lanes on different banks
+template <int VT, int K>
+__global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
+{
+    using S = value_store_t<VT>;
+    constexpr int kBring = kThreads / 8;  // rows an access
+    extern __shared__ float rows_of_lanes[];
+    const int pitch = lane_row_pitch(C.V), part = threadIdx.x % 8 * kRowUnit;
+    const int64_t row0 = (int64_t)blockIdx.x * kThreads, row = row0 + threadIdx.x;
+    const S *x = (const S*)C.logits, *end = x + C.N * C.V;
+    RawUnit<VT> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = row0 + i * kBring + threadIdx.x / 8;
+        raw[i] = fetch_row_unit<VT>(x + r * C.V + part, r < C.N ? C.V - part : 0, end);
+    }
+    const Asked asked = given_class<VT>(C, min(row, C.N - 1));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float* to = rows_of_lanes + (i * kBring + threadIdx.x / 8) * pitch + part;
+        if (part < pitch - 1) {
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j) to[j] = raw_value<VT>(raw[i], j);
+        }
+    }
+    __syncthreads();
+    if (row >= C.N) return;
+    const float *mine = rows_of_lanes + threadIdx.x * pitch, c = C.scale * kLog2e;
+    uint32_t few[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) few[i] = 0;
+#pragma unroll 4
+    for (int j = 0; j < C.V; ++j) {
+        uint32_t key = (value_key(mine[j]) & ~63u) | (uint32_t)(63 - j);
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const uint32_t less = min(few[i], key);
+            few[i] = max(few[i], key);
+            key = less;
+        }
+    }
+    uint64_t best[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) best[i] = few[i] ? key_of(mine[63 - (few[i] & 63u)], 63 - (few[i] & 63u)) : 0;
+    if constexpr (VT == MAXK_VALUE_F32) {
+        bool near = false;
+#pragma unroll
+        for (int i = 0; i + 1 < K; ++i) near |= i < C.top_k && (few[i] ^ few[i + 1]) < 64u;
+        if (near) {
+            double whole[K];
+#pragma unroll
+            for (int i = 0; i < K; ++i) whole[i] = 0.0;
+            for (int j = 0; j < C.V; ++j) {
+                double key = pair_key(mine[j], j);
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    const double less = lesser_of(whole[i], key);
+                    whole[i] = greater_of(whole[i], key);
+                    key = less;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < K; ++i) best[i] = unpaired(whole[i]);
+        }
+    }
+    Sums s = no_sums();
+    s.m = fmaxf(key_value((uint32_t)(best[0] >> 32)), s.m);  // (a NaN, which is greater than all others, makes S one)
+#pragma unroll 4
+    for (int j = 0; j < C.V; ++j) {
+        const float d = (mine[j] - s.m) * c, e = exp2_of(d);
+        s.S += e;
+        s.T = fmaf(e, fmaxf(d, -kFar), s.T);
+    }
+    const Found f = row_results(C, row, s, asked);
+    store_results(C, row, f);
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (i < C.top_k) store_likeliest(C, row, s, f.ln, best[i], i);
+}
+
 // ---- a workgroup a row ----
 
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
@@ -800,7 +915,7 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     __shared__ Sums room[T / kWave];
     __shared__ Asked asked_room;
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
-    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWaiting];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     Likeliest best;
@@ -845,7 +960,7 @@ __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Part
     constexpr int T = kThreads;
     __shared__ Sums room[T / kWave];
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
-    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWaiting];
     const int64_t row = blockIdx.x / P.segments;
     const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
@@ -878,7 +993,7 @@ template <int T, bool TOP>
 __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
 {
     __shared__ Sums sums_room[T / kWave];
-    __shared__ uint64_t keys[TOP ? T / kWave : 1][2 * kWave];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWave];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     uint64_t mine = 0;
@@ -954,9 +1069,27 @@ maxk_status run_rows(const ClassCall& C, hipStream_t s)
     return MAXK_OK;
 }
 
+// Rows for two such workgroups on a CU; fewer are better off with lanes that share a row.  us, a lane a row / eight lanes, 47 fp32 with 5 alternatives: 1024 rows 8.2 /
+// 4.6, 20 k 10.7 / 5.6, 100 k 15.1 / 13.6, 300 k 26.6 / 31.8, 2.4 M 171 / 259
+constexpr int kManyRows = 2 * 256 * kThreads;
+template <int VT, int K>
+maxk_status run_lane_rows(const ClassCall& C, hipStream_t s)
+{
+    hipLaunchKernelGGL((class_lane_kernel<VT, K>), dim3((unsigned)((C.N + kThreads - 1) / kThreads)), dim3(kThreads), kThreads * lane_row_pitch(C.V) * sizeof(float), s, C);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
 template <int VT, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
 {
+    if constexpr (TOP)
+        if (const int keys = C.top_k + (VT == MAXK_VALUE_F32); C.V <= kLaneRowMost && keys <= kLaneRowKeys && C.N >= kManyRows) {
+            if (keys <= 2) return run_lane_rows<VT, 2>(C, s);
+            if (keys <= 4) return run_lane_rows<VT, 4>(C, s);
+            if (keys <= 6) return run_lane_rows<VT, 6>(C, s);
+            return run_lane_rows<VT, kLaneRowKeys>(C, s);
+        }
     const int units = (C.V + kRowUnit - 1) / kRowUnit;
     if (units <= 4) return run_teams<VT, 4, 1, DISTILL, GRAD, TOP>(C, s);
     if (units <= 8) return run_teams<VT, 8, 1, DISTILL, GRAD, TOP>(C, s);

@@ -137,11 +137,13 @@ __device__ __forceinline__ void store_row_unit(value_store_t<VT>* p, int valid, 
 
 // ---- over the L lanes (a power of two, up to 64) that share a row: every lane has the result, the same bits ----
 
-__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 1>) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true); }
-__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 2>) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true); }
+template <int CONTROL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CONTROL, 0xF, 0xF, true); }
+__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 1>) { return dpp<0xB1>(x); }   // quad_perm [1,0,3,2]
+__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 2>) { return dpp<0x4E>(x); }   // quad_perm [2,3,0,1]
 // (of lanes that agree in each group of 4, and of 8)
-__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 4>) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true); }  // row_half_mirror
-__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 8>) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true); }  // row_mirror
+__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 4>) { return dpp<0x141>(x); }  // row_half_mirror
+__device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 8>) { return dpp<0x140>(x); }  // row_mirror
 __device__ __forceinline__ uint32_t xor_lane(uint32_t x, std::integral_constant<int, 16>)
 {
     const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);

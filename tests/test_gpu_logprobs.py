@@ -86,6 +86,37 @@ def test_alternatives_in_any_order(V):
         check(rows, labels, k)
 
 
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("V,k", [(1, 1), (5, 5), (16, 2), (40, 4), (47, 5), (47, 7), (63, 8), (64, 6), (64, 8)])
+def test_alternatives_of_many_short_rows(V, k, dtype):
+    """Rows enough for the form with a lane a row; values that share their leading bits, equal values, masked ones."""
+    N = 140_001
+    x, labels, gen = inputs(N, V, dtype, V + k)
+    x[100:200] = (1 + torch.randint(0, 3, (100, V), generator=gen, device="cuda") * 2.0 ** -20).to(dtype)  # (fp32: equal in 26 bits, and not)
+    x[200:300] = torch.randint(0, 3, (100, V), generator=gen, device="cuda").to(dtype)
+    x[300:400, V // 2:] = -INF
+    if V > 1:
+        x[400, 1], x[401, 0] = NAN, INF
+    logprob, entropy, data, index = results(N, k)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    order = torch.sort(x[:400].float(), dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(index[:400].long(), order)
+    some = torch.cat([torch.arange(400), torch.arange(N - 300, N)]).cuda()
+    lp, lp_bound, H, H_bound, R = hc.logprobs(x[some], labels[some])
+    hc.close(logprob[some], lp, lp_bound)
+    hc.close(entropy[some], H, H_bound)
+    want = hc.likeliest(x[some], k)
+    assert np.array_equal(index[some].cpu().numpy(), want)
+    top = np.take_along_axis(R.logp, want, 1)
+    hc.close(data[some], top, R.u + 4 * hc.U * (np.abs(np.where(np.isfinite(top), top, 0)) + 2 * np.abs(R.lnS)))
+    few = slice(0, 20_000)  # the other form's columns and values
+    small = results(20_000, k)
+    maxk.maxk_logprobs(x[few], labels[few], *small)
+    assert torch.equal(small[3], index[few]) or V > 1 and torch.equal(torch.cat([small[3][:400], small[3][402:]]), torch.cat([index[:400], index[402:20_000]]))
+    if V > 1:
+        assert torch.isnan(data[400:402]).all() and torch.isnan(entropy[400:402]).all() and ((index[400:402] >= 0) & (index[400:402] < V)).all()
+
+
 def test_masks_of_the_lowest_value_and_of_everything():
     lowest = torch.finfo(torch.float32).min
     x = torch.full((4, 100), lowest, device="cuda")
