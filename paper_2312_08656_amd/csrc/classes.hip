@@ -178,7 +178,8 @@ __device__ __forceinline__ uint64_t merge_waves(uint64_t mine, uint64_t (&keys)[
 }
 
 // A wavefront's greatest keys: in falling order over the lanes, and those that wait in LDS to be sorted in.  A unit whose largest value is below the k-th
-// greatest key costs a comparison.
+// greatest key costs a comparison.  Classes that are masked out (-Inf) are left out, and come in when a row has fewer than k others (fill): a masked
+// stretch of a vocabulary would be all equal keys.
 struct Likeliest {
     uint64_t mine, least;   // least: of a key that is still wanted (it is greater)
     float least_value;
@@ -224,7 +225,7 @@ struct Likeliest {
     // offered.  (any: the lane has one)
     __device__ __forceinline__ void expect(float top, bool any)
     {
-        const uint32_t key = any ? value_key(top) : 0u;
+        const uint32_t key = any && top > -__builtin_inff() ? value_key(top) : 0u;
         uint32_t bound = 0;
 #pragma unroll
         for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1)
@@ -234,10 +235,10 @@ struct Likeliest {
     // a unit at column `col`: all lanes come here, those without columns with valid < 1
     __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid)
     {
-        if (!__any(valid > 0 && top >= least_value)) return;
+        if (!__any(valid > 0 && top >= least_value && top > -__builtin_inff())) return;
 #pragma unroll
         for (int j = 0; j < kRowUnit; ++j) {
-            const bool perhaps = j < valid && x[j] >= least_value;
+            const bool perhaps = j < valid && x[j] >= least_value && x[j] > -__builtin_inff();
             if (!__any(perhaps)) continue;
             const uint64_t key = key_of(x[j], (uint32_t)(col + j));
             const bool wanted = perhaps && key > least;
@@ -249,6 +250,25 @@ struct Likeliest {
     }
     __device__ __forceinline__ void end() { while (waiting > 0) sort_in(); }
 };
+
+// The keys of a row in falling order, filled up to k with its first masked columns where there are fewer.  (room: k keys in LDS of the wavefront)
+template <int VT>
+__device__ __forceinline__ uint64_t fill(uint64_t key, const value_store_t<VT>* x, int V, int k, int lane, uint64_t* room)
+{
+    int have = __popcll(__ballot(lane < k && key));
+    if (have >= k) return key;
+    const int found = have;
+    for (int base = 0; base < V && have < k; base += kWave) {
+        const int col = base + lane;
+        const bool masked = col < V && widen_value<VT>(x[col]) == -__builtin_inff();
+        const uint64_t who = __ballot(masked);
+        const int at = have + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+        if (masked && at < k) room[at] = key_of(-__builtin_inff(), (uint32_t)col);
+        have += __popcll(who);
+    }
+    wave_fence();
+    return lane >= found && lane < min(have, k) ? room[lane] : key;
+}
 
 // ---- a row ----
 
@@ -773,7 +793,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
             best.offer(v[u], largest(v[u]), col, C.V - col);
         }
         best.end();
-        store_likeliest(C, row, s, f.ln, best.mine, lane);
+        store_likeliest(C, row, s, f.ln, fill<VT>(best.mine, x, C.V, C.top_k, lane, keys[team]), lane);
     } else if constexpr (TOP) {
         static_assert(U == 1);
         double key[kRowUnit];
@@ -935,7 +955,8 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     if constexpr (TOP) {
         best.end();
         const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
-        if (wave == 0) store_likeliest(C, row, s, f.ln, key, lane);
+        if (wave == 0)
+            store_likeliest(C, row, s, f.ln, fill<VT>(key, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
     }
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (GRAD) {
@@ -989,7 +1010,7 @@ __device__ __forceinline__ Sums join_segments(const ClassCall& C, const Parts& P
     return join_workgroup<T>(s, C.scale * kLog2e, room);
 }
 
-template <int T, bool TOP>
+template <int VT, int T, bool TOP>
 __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
 {
     __shared__ Sums sums_room[T / kWave];
@@ -1005,7 +1026,8 @@ __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
     const Found f = row_results(C, row, s, P.asked[row]);
     if constexpr (TOP) {
         mine = merge_waves<T>(mine, keys, lane, wave);
-        if (wave == 0) store_likeliest(C, row, s, f.ln, mine, lane);
+        if (wave == 0)
+            store_likeliest(C, row, s, f.ln, fill<VT>(mine, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
     }
     if (threadIdx.x == 0) store_results(C, row, f);
 }
@@ -1117,7 +1139,7 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     hipLaunchKernelGGL((class_parts_kernel<VT, DISTILL, TOP>), dim3(groups), dim3(kThreads), 0, s, C, P);
     MAXK_LAUNCH_CHECK();
     if constexpr (GRAD) hipLaunchKernelGGL((class_gradient_kernel<VT, DISTILL>), dim3(groups), dim3(kThreads), 0, s, C, P);
-    else hipLaunchKernelGGL((class_join_kernel<TOP ? 1024 : kThreads, TOP>), dim3((unsigned)C.N), dim3(TOP ? 1024 : kThreads), 0, s, C, P);
+    else hipLaunchKernelGGL((class_join_kernel<VT, TOP ? 1024 : kThreads, TOP>), dim3((unsigned)C.N), dim3(TOP ? 1024 : kThreads), 0, s, C, P);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
