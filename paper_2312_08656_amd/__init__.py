@@ -58,4 +58,17 @@ from .heads import (  # noqa: E402,F401
     maxk_rms_norm_grad,
     rms_norm_grad_workspace,
 )
-from .autograd import MaxKAggregate, MaxKLayer, maxk_aggregate, maxk_layer  # noqa: E402,F401
+from .autograd import (  # noqa: E402,F401
+    MaxKAggregate,
+    MaxKDistill,
+    MaxKLayer,
+    MaxKLogprobs,
+    MaxKNormLayer,
+    MaxKRMSNorm,
+    maxk_aggregate,
+    maxk_class_logprobs,
+    maxk_distill_loss,
+    maxk_layer,
+    maxk_norm_layer,
+    maxk_residual_norm,
+)
