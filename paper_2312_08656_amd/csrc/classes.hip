@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256;  // of a workgroup; T below: 256 or 1024
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr auto kNothing = [] {};
 constexpr float kFar = 256.f;  // 2^-256 is 0 in fp32: a difference past it need not be told, and is cut so that 0 times it stays 0
 
 // Of a part of a row: its largest value (the lowest fp32 value where it has none above), S and T.  -Inf adds 0, NaN and +Inf make S a NaN.
@@ -299,24 +300,47 @@ struct Entries {  // of the teacher, in LDS
 
 constexpr auto kMax = [](float a, float b) { return fmaxf(a, b); };
 
-// Of several entries of a column the first one has their sum.  Few entries are seen to by the wavefront that takes them, while the others go through the row; more
-// by all threads in the end.
-constexpr int kFewEntries = 2 * kWave;
-__device__ __forceinline__ void sum_of_column(const ClassCall& C, const Entries& E, int i, float& sum, bool& mine)
-{
-    sum = 0.f;
-    mine = i < C.k;
-    const int col = mine ? E.col[i] : -1;
-    for (int j = 0; j < C.k; ++j)
-        if (E.col[j] == col) {
-            mine &= j >= i;
-            sum += E.q[j];
-        }
-}
+// The teacher's entries of a row by one wavefront, while the others go through the row: their q and the student's x there.  An entry whose column lies outside the
+// row is none.  Of several entries of a column the first one has their sum, in the entries' order; where there are more entries than lanes all threads see to that
+// in the end.
+constexpr int kFewEntries = kWave;
 
-// The teacher's entries of a row by one wavefront: their q and the student's x there.  An entry whose column lies outside the row is none.
 template <int VT>
-__device__ Asked take_entries(const ClassCall& C, int64_t row, int lane, Entries& E)
+struct FewEntries {  // up to one a lane; asked for before the row is gone through, and seen to behind it
+    int col;
+    float t, v;
+    __device__ __forceinline__ void ask(const ClassCall& C, int64_t row, int lane)
+    {
+        const int64_t at = lane < C.k ? column_of(C, row * C.k + lane) : -1;
+        const bool there = at >= 0 && at < C.V;
+        col = there ? (int)at : -1;
+        t = there ? teacher_value(C, row * C.k + lane) : -__builtin_inff();
+        v = there ? widen_value<VT>(((const value_store_t<VT>*)C.logits)[row * C.V + col]) : -__builtin_inff();
+    }
+    __device__ __forceinline__ Asked take(const ClassCall& C, int lane, bool gradient, Entries& E)
+    {
+        const float c = C.scale * kLog2e, top = over_lanes<kWave>(fmaxf(t, kLowest), kMax), ref = over_lanes<kWave>(fmaxf(v, kLowest), kMax);
+        const float d = (t - top) * c, e = exp2_of(d), sum = over_lanes<kWave>(e, kAdd), inverse = 1.f / sum;
+        float q = sum == 0.f ? 0.f : e * inverse;
+        const float loss = over_lanes<kWave>(q != 0.f ? q * (fmaf(kLn2, d, -logf(sum)) - (v - ref) * C.scale) : 0.f, kAdd);
+        if (gradient) {
+            float all = 0.f;
+            bool mine = true;
+#pragma unroll 4
+            for (int j = 0; j < C.k; ++j) {
+                const bool same = __builtin_amdgcn_readlane(col, j) == col;
+                all += same ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(q), j)) : 0.f;
+                mine &= !same || j >= lane;
+            }
+            q = all;
+            if (lane < C.k) E.col[lane] = mine ? col : -1, E.q[lane] = q, E.x[lane] = v;
+        }
+        return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
+    }
+};
+
+template <int VT>
+__device__ Asked take_more_entries(const ClassCall& C, int64_t row, int lane, Entries& E)
 {
     const value_store_t<VT>* x = (const value_store_t<VT>*)C.logits + row * C.V;
     float top = kLowest, ref = kLowest;
@@ -342,21 +366,18 @@ __device__ Asked take_entries(const ClassCall& C, int64_t row, int lane, Entries
         if (q != 0.f) loss += q * (fmaf(kLn2, d, -ln) - (E.x[i] - ref) * C.scale);
         E.q[i] = q;
     }
-    if (C.dlogits && C.k <= kFewEntries) {
-        wave_fence();
-        float all[kFewEntries / kWave];
-        bool mine[kFewEntries / kWave];
-#pragma unroll
-        for (int r = 0; r < kFewEntries / kWave; ++r) sum_of_column(C, E, lane + r * kWave, all[r], mine[r]);
-        wave_fence();
-#pragma unroll
-        for (int r = 0; r < kFewEntries / kWave; ++r)
-            if (const int i = lane + r * kWave; i < C.k) {
-                E.q[i] = all[r];
-                if (!mine[r]) E.col[i] = -1;
-            }
-    }
     return {0.f, over_lanes<kWave>(loss, kAdd), ref, sum == 0.f ? 0.f : sum * inverse};
+}
+
+__device__ __forceinline__ void sum_of_column(const ClassCall& C, const Entries& E, int i, float& sum, bool& mine)
+{
+    sum = 0.f;
+    const int col = E.col[i];
+    for (int j = 0; j < C.k; ++j)
+        if (E.col[j] == col) {
+            mine &= j >= i;
+            sum += E.q[j];
+        }
 }
 
 template <int VT>
@@ -508,11 +529,13 @@ __device__ __forceinline__ Sums sum_columns(const ClassCall& C, int64_t row, int
 __device__ __forceinline__ bool far_off(const Sums& s, float c) { return !(fabsf(s.m * c) < kFarOff); }
 
 // The workgroup's sums of these columns (`room` is free behind the next barrier); what other wavefronts left in LDS before is there
-template <int VT, int T, bool ENTROPY, bool TOP>
-__device__ __forceinline__ Sums sum_row(const ClassCall& C, int64_t row, int first, int last, Likeliest& best, Sums* room)
+template <int VT, int T, bool ENTROPY, bool TOP, typename F>
+__device__ __forceinline__ Sums sum_row(const ClassCall& C, int64_t row, int first, int last, Likeliest& best, Sums* room, F&& before_joining)
 {
     const float c = C.scale * kLog2e;
-    Sums s = join_workgroup<T>(sum_columns<VT, T, false, ENTROPY, TOP>(C, row, first, last, best), c, room);
+    Sums s = sum_columns<VT, T, false, ENTROPY, TOP>(C, row, first, last, best);
+    before_joining();
+    s = join_workgroup<T>(s, c, room);
     if (far_off(s, c)) {
         s = sum_columns<VT, T, true, ENTROPY, false>(C, row, first, last, best);
         __syncthreads();
@@ -522,8 +545,8 @@ __device__ __forceinline__ Sums sum_row(const ClassCall& C, int64_t row, int fir
 }
 
 // Their gradient; distillation's entries in these columns follow
-template <int VT, int T, bool CAREFUL, bool DISTILL>
-__device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
+template <int VT, int T, bool CAREFUL, bool DISTILL, typename F>
+__device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E, F&& before_entries)
 {
     using S = value_store_t<VT>;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
@@ -563,6 +586,7 @@ __device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, i
             unit(v, col);
             store_row_unit<VT>(dx + col, valid, v);
         });
+    before_entries();
     if constexpr (DISTILL) {
         __syncthreads();  // what is stored above at their columns is stored again
         for (int i = threadIdx.x; i < C.k; i += T) {
@@ -576,11 +600,11 @@ __device__ __forceinline__ void store_columns(const ClassCall& C, int64_t row, i
     }
 }
 
-template <int VT, int T, bool DISTILL>
-__device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E)
+template <int VT, int T, bool DISTILL, typename F>
+__device__ __forceinline__ void store_gradient(const ClassCall& C, int64_t row, int first, int last, const Sums& s, const Slope& k, const Entries* E, F&& before_entries)
 {
-    if (far_off(s, C.scale * kLog2e)) store_columns<VT, T, true, DISTILL>(C, row, first, last, s, k, E);
-    else store_columns<VT, T, false, DISTILL>(C, row, first, last, s, k, E);
+    if (far_off(s, C.scale * kLog2e)) store_columns<VT, T, true, DISTILL>(C, row, first, last, s, k, E, before_entries);
+    else store_columns<VT, T, false, DISTILL>(C, row, first, last, s, k, E, before_entries);
 }
 
 // ---- a row in the registers of L lanes, U units of 8 columns each ----
@@ -653,31 +677,73 @@ struct TeamEntries {
     __device__ __forceinline__ Asked take()
     {
         const float c = C.scale * kLog2e;
-        return C.k <= L ? take_one(c) : take_more(c);
+        if (C.k <= L) return take_some<1>(c);
+        if (C.k <= 4 * L) return take_some<4>(c);
+        if (U == 1 || C.k <= 8 * L) return take_some<8>(c);  // (no row has more columns)
+        return take_more(c);
     }
 
-    __device__ __forceinline__ Asked take_one(float c)
+    template <int R>
+    __device__ __forceinline__ Asked take_some(float c)  // up to R entries a lane
     {
-        const float xs = logit(first), top = over_lanes<L>(fmaxf(own, kLowest), kMax), ref = over_lanes<L>(fmaxf(xs, kLowest), kMax);
-        const float d = (own - top) * c, e = exp2_of(d), sum = over_lanes<L>(e, kAdd), ln = logf(sum), inverse = 1.f / sum;
-        float q = sum == 0.f ? 0.f : e * inverse;
-        const float loss = over_lanes<L>(q != 0.f ? q * (fmaf(kLn2, d, -ln) - (xs - ref) * C.scale) : 0.f, kAdd);
+        int col[R];
+        float t[R], v[R], q[R], top = kLowest, ref = kLowest;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = lane + r * L;
+            col[r] = R == 1 ? first : i < C.k ? column(i) : -1;
+            t[r] = R == 1 ? own : value(i, col[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            v[r] = logit(col[r]);
+            top = fmaxf(top, t[r]);
+        }
+        top = over_lanes<L>(top, kMax);
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            t[r] = (t[r] - top) * c;
+            q[r] = exp2_of(t[r]);
+            sum += q[r];
+            ref = fmaxf(ref, v[r]);
+        }
+        sum = over_lanes<L>(sum, kAdd);
+        ref = over_lanes<L>(ref, kMax);
+        const float ln = logf(sum), inverse = 1.f / sum;
+        float loss = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            q[r] = sum == 0.f ? 0.f : q[r] * inverse;
+            loss += q[r] != 0.f ? q[r] * (fmaf(kLn2, t[r], -ln) - (v[r] - ref) * C.scale) : 0.f;
+        }
+        loss = over_lanes<L>(loss, kAdd);
         if constexpr (GRAD) {
             clear();
-            if (first >= 0) spread[first] = __int_as_float(lane + 1);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (col[r] >= 0) spread[col[r]] = __int_as_float(lane + r * L + 1);
             wave_fence();
-            const bool other = others(lane, first);
-            if (any(other)) {  // sums in the entries' order
-                float all = 0.f;
-                for (int j = 0; j < C.k; ++j) {
-                    const int col = __shfl(first, j, L);
-                    const float p = __shfl(q, j, L);
-                    all += col == first ? p : 0.f;
-                }
-                q = all;
+            uint32_t other = 0;  // entries that are not the one that writes their column
+#pragma unroll
+            for (int r = 0; r < R; ++r) other |= (uint32_t)others(lane + r * L, col[r]) << r;
+            if (any(other != 0)) {  // sums in the entries' order
+                float all[R] = {};
+#pragma unroll
+                for (int from = 0; from < R; ++from)
+                    for (int l = 0; l < L; ++l) {
+                        const int there = __shfl(col[from], l, L);
+                        const float p = __shfl(q[from], l, L);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) all[r] += there == col[r] ? p : 0.f;
+                    }
+#pragma unroll
+                for (int r = 0; r < R; ++r) q[r] = all[r];
             }
             wave_fence();
-            if (first >= 0 && !other) spread[first] = q;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (col[r] >= 0 && !(other >> r & 1)) spread[col[r]] = q[r];
             wave_fence();
         }
         return {0.f, loss, ref, sum == 0.f ? 0.f : sum * inverse};
@@ -734,6 +800,64 @@ struct TeamEntries {
     }
 };
 
+template <int L>
+__device__ __forceinline__ void likeliest_in_turn(const ClassCall& C, int64_t row, const Sums& s, float ln, const float (&v)[kRowUnit], int lane)
+{
+    double key[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) key[j] = lane * kRowUnit + j < C.V ? pair_key(v[j], lane * kRowUnit + j) : 0.0;
+    double taken = 0.0;
+    for (int i = 0; i < C.top_k; ++i) {
+        double best = key[0];
+#pragma unroll
+        for (int j = 1; j < kRowUnit; ++j) best = greater_of(best, key[j]);
+        best = over_lanes<L>(best, [](double a, double b) { return greater_of(a, b); });
+        const int col = (int)(0xFFFFFu - ((uint32_t)__double2loint(best) & 0xFFFFFu));
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j)
+            if (col == lane * kRowUnit + j) key[j] = __hiloint2double(0, __double2loint(key[j]));
+        if (i % L == lane) taken = best;
+        if (i % L == L - 1 || i == C.top_k - 1) {
+            const int at = i - i % L + lane;
+            if (at <= i) store_likeliest(C, row, s, ln, unpaired(taken), at);
+        }
+    }
+}
+
+// A column's place is the number of columns with a greater value, or an equal one to the left of it: of those to the left a value counts that is greater than this one's
+// key less 1.  (room: the row's keys in LDS.  Keys from 1 on: 0 is behind the row's end)
+template <int L>
+__device__ __forceinline__ void likeliest_by_place(const ClassCall& C, int64_t row, const Sums& s, float ln, const float (&v)[kRowUnit], int lane, uint32_t* room)
+{
+    uint32_t key[kRowUnit];
+    int place[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) {
+        key[j] = lane * kRowUnit + j < C.V ? max(value_key(v[j]), 1u) : 0u;
+        place[j] = 0;
+    }
+    *reinterpret_cast<uint4*>(room + lane * kRowUnit) = make_uint4(key[0], key[1], key[2], key[3]);
+    *reinterpret_cast<uint4*>(room + lane * kRowUnit + 4) = make_uint4(key[4], key[5], key[6], key[7]);
+    wave_fence();
+    for (int part = 0; part * kRowUnit < C.V; ++part) {
+        const uint4 a = *reinterpret_cast<const uint4*>(room + part * kRowUnit), b = *reinterpret_cast<const uint4*>(room + part * kRowUnit + 4);
+        const uint32_t other[kRowUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) {
+            const uint32_t over = part < lane ? key[j] - 1u : part > lane ? key[j] : 0xFFFFFFFFu;  // (its own columns: below)
+#pragma unroll
+            for (int i = 0; i < kRowUnit; ++i) place[j] += other[i] > over;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j)
+#pragma unroll
+        for (int i = 0; i < kRowUnit; ++i) place[j] += i < j ? key[i] >= key[j] : key[i] > key[j];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j)
+        if (lane * kRowUnit + j < C.V && place[j] < C.top_k) store_likeliest(C, row, s, ln, key_of(v[j], (uint32_t)(lane * kRowUnit + j)), place[j]);
+}
+
 struct Nothing {
     __device__ __forceinline__ Nothing(const ClassCall&, int64_t, int, float*) {}
 };
@@ -745,6 +869,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     constexpr int kTeams = kThreads / L;
     __shared__ __attribute__((aligned(16))) float spread[DISTILL && GRAD ? kTeams * L * U * kRowUnit : 1];
     __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? kWaiting : 1];
+    __shared__ __attribute__((aligned(16))) uint32_t places[TOP && L < kWave ? kThreads * kRowUnit : 1];
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t row = (int64_t)blockIdx.x * kTeams + team;
     if (row >= C.N) return;
@@ -796,25 +921,9 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         store_likeliest(C, row, s, f.ln, fill<VT>(best.mine, x, C.V, C.top_k, lane, keys[team]), lane);
     } else if constexpr (TOP) {
         static_assert(U == 1);
-        double key[kRowUnit];
-#pragma unroll
-        for (int j = 0; j < kRowUnit; ++j) key[j] = lane * kRowUnit + j < C.V ? pair_key(v[0][j], lane * kRowUnit + j) : 0.0;
-        double taken = 0.0;
-        for (int i = 0; i < C.top_k; ++i) {
-            double best = key[0];
-#pragma unroll
-            for (int j = 1; j < kRowUnit; ++j) best = greater_of(best, key[j]);
-            best = over_lanes<L>(best, [](double a, double b) { return greater_of(a, b); });
-            const int col = (int)(0xFFFFFu - ((uint32_t)__double2loint(best) & 0xFFFFFu));
-#pragma unroll
-            for (int j = 0; j < kRowUnit; ++j)
-                if (col == lane * kRowUnit + j) key[j] = __hiloint2double(0, __double2loint(key[j]));
-            if (i % L == lane) taken = best;
-            if (i % L == L - 1 || i == C.top_k - 1) {
-                const int at = i - i % L + lane;
-                if (at <= i) store_likeliest(C, row, s, f.ln, unpaired(taken), at);
-            }
-        }
+        // Few alternatives in rounds, some fifty instructions each; many by their places, 18 instructions a column.  us, 27685 rows of 41 bf16 with all of them, 21 / 12
+        if (3 * C.top_k < C.V) likeliest_in_turn<L>(C, row, s, f.ln, v[0], lane);
+        else likeliest_by_place<L>(C, row, s, f.ln, v[0], lane, places + team * L * kRowUnit);
     }
     if constexpr (GRAD) {
         const Slope k = row_slope(C, row, s, asked, f);
@@ -942,14 +1051,16 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
     Asked asked;
     if constexpr (DISTILL) {
-        if (wave == 0) {
-            asked = take_entries<VT>(C, row, lane, entries);
+        if (wave == 0) {  // (before its share of the row: the other wavefronts are on their way)
+            FewEntries<VT> few;
+            if (C.k <= kFewEntries) few.ask(C, row, lane), asked = few.take(C, lane, GRAD, entries);
+            else asked = take_more_entries<VT>(C, row, lane, entries);
             if (lane == 0) asked_room = asked;
         }
     } else {
         asked = given_class<VT>(C, row);
     }
-    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, 0, C.V, best, room);
+    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, 0, C.V, best, room, kNothing);
     if constexpr (DISTILL) asked = asked_room;
     const Found f = row_results(C, row, s, asked);
     if constexpr (TOP) {
@@ -961,8 +1072,8 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (GRAD) {
         const Slope k = row_slope(C, row, s, asked, f);
-        if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, 0, C.V, s, k, &entries);
-        else store_gradient<VT, T, false>(C, row, 0, C.V, s, k, nullptr);
+        if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, 0, C.V, s, k, &entries, kNothing);
+        else store_gradient<VT, T, false>(C, row, 0, C.V, s, k, nullptr, kNothing);
     }
 }
 
@@ -987,13 +1098,18 @@ __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Part
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     Likeliest best;
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
-    if (segment == 0 && wave == 0) {
-        Asked asked;
-        if constexpr (DISTILL) asked = take_entries<VT>(C, row, lane, entries);
-        else asked = given_class<VT>(C, row);
-        if (lane == 0) P.asked[row] = asked;
+    const bool asks = segment == 0 && wave == 0;
+    Asked asked;
+    FewEntries<VT> few;
+    if (asks) {
+        if constexpr (!DISTILL) asked = given_class<VT>(C, row);
+        else if (C.k <= kFewEntries) few.ask(C, row, lane);
     }
-    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, first, last, best, room);
+    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, first, last, best, room, [&] {
+        if (!asks) return;
+        if constexpr (DISTILL) asked = C.k <= kFewEntries ? few.take(C, lane, false, entries) : take_more_entries<VT>(C, row, lane, entries);
+        if (lane == 0) P.asked[row] = asked;
+    });
     if (threadIdx.x == 0) P.sums[blockIdx.x] = s;
     if constexpr (TOP) {
         best.end();
@@ -1041,15 +1157,23 @@ __global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, P
     const int64_t row = blockIdx.x / P.segments;
     const int segment = blockIdx.x % P.segments, first = segment * P.width, last = min(first + P.width, C.V);
     // (x of other segments may have been overwritten: of the entries only those of this one are used)
-    if constexpr (DISTILL)
-        if (threadIdx.x < kWave) take_entries<VT>(C, row, threadIdx.x, entries);
+    FewEntries<VT> few;
+    if constexpr (DISTILL) {
+        if (threadIdx.x < kWave) {
+            if (C.k <= kFewEntries) few.ask(C, row, threadIdx.x);
+            else take_more_entries<VT>(C, row, threadIdx.x, entries);
+        }
+    }
     const Sums s = join_segments<T>(C, P, row, room);
     const Asked asked = P.asked[row];
     const Found f = row_results(C, row, s, asked);
     if (segment == 0 && threadIdx.x == 0) store_results(C, row, f);
     const Slope k = row_slope(C, row, s, asked, f);
-    if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, first, last, s, k, &entries);
-    else store_gradient<VT, T, false>(C, row, first, last, s, k, nullptr);
+    if constexpr (DISTILL)
+        store_gradient<VT, T, true>(C, row, first, last, s, k, &entries, [&] {
+            if (threadIdx.x < kWave && C.k <= kFewEntries) few.take(C, threadIdx.x, true, entries);
+        });
+    else store_gradient<VT, T, false>(C, row, first, last, s, k, nullptr, kNothing);
 }
 
 // Threads of a workgroup that has a row.  The gradient reads its rows again: those that all CUs work on at a time have to stay in the Infinity Cache.
@@ -1063,10 +1187,11 @@ int threads_of(int V)
 // Segments of a row
 struct Cut { int segments, width; };
 constexpr int kLeastSegment = kThreads * kRowUnit;
+constexpr int kFewRows = 128;  // fewer are cut, up to 256 workgroups take 1024 threads a row
 Cut cut_of(int64_t N, int V)
 {
     constexpr int kGroups = 512;
-    if (N >= kGroups || V < 2 * kLeastSegment) return {1, V};
+    if (N >= kFewRows || V < 8 * kLeastSegment) return {1, V};
     const int most = (V + kLeastSegment - 1) / kLeastSegment, wanted = (int)((kGroups + N - 1) / std::max<int64_t>(N, 1));
     const int per = (most + std::min(most, wanted) - 1) / std::min(most, wanted);
     return {(most + per - 1) / per, per * kLeastSegment};
@@ -1122,11 +1247,9 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
     if (cut.segments == 1) {
-        const int T = GRAD ? threads_of<VT>(C.V) : kThreads;
-        if constexpr (GRAD) {
-            if (T == 1024) return run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s);
-            if (T == 512) return run_rows<VT, 512, DISTILL, GRAD, TOP>(C, s);
-        }
+        const int T = C.N <= 512 && C.V >= 2 * kLeastSegment ? 1024 : C.N <= 1024 && C.V >= 2 * kLeastSegment ? 512 : GRAD ? threads_of<VT>(C.V) : kThreads;
+        if (T == 1024) return run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s);
+        if (T == 512) return run_rows<VT, 512, DISTILL, GRAD, TOP>(C, s);
         return run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);
     }
     char* at = (char*)workspace;

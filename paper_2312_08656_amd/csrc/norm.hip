@@ -227,7 +227,7 @@ int64_t grad_groups(int64_t N, int dim)
 {
     const int teams = teams_of(row_form(dim));
     const int64_t all = (N + teams - 1) / teams, resident = 4 * 256 * kThreads / norm_threads(row_form(dim).lanes);
-    return std::min({all, resident, std::max<int64_t>(256, N / 8)});
+    return all <= 4 ? 1 : std::min({all, resident, std::max<int64_t>(256, N / 8)});  // (a few rounds of one workgroup cost less than a second launch)
 }
 
 template <int VT>
