@@ -1126,26 +1126,58 @@ __device__ __forceinline__ Sums join_segments(const ClassCall& C, const Parts& P
     return join_workgroup<T>(s, C.scale * kLog2e, room);
 }
 
+// The likeliest of the segments' lists: keys no less than the k-th greatest of the lists' first ones (of 64 sets of lists) are few, and each counts those that are greater.
+// Where they are many (equal values), wavefronts merge the lists.
+constexpr int kCandidates = 1024;
 template <int VT, int T, bool TOP>
 __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
 {
     __shared__ Sums sums_room[T / kWave];
-    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWave];
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWave];  // (16 x 64: room for the candidates)
+    __shared__ int candidates;
+    static_assert(!TOP || T == kCandidates);
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
-    uint64_t mine = 0;
     if constexpr (TOP) {
-        for (int i = wave; i < P.segments; i += T / kWave)
-            mine = merge_keys(mine, lane < C.top_k ? P.keys[(row * P.segments + i) * C.top_k + lane] : 0, lane);
+        if (threadIdx.x == 0) candidates = 0;
     }
     const Sums s = join_segments<T>(C, P, row, sums_room);
     const Found f = row_results(C, row, s, P.asked[row]);
+    if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (TOP) {
+        const uint64_t* all = P.keys + row * P.segments * C.top_k;
+        const int n = P.segments * C.top_k;
+        uint32_t head = 0;
+        for (int i = lane; i < P.segments; i += kWave) head = max(head, (uint32_t)(all[(int64_t)i * C.top_k] >> 32));
+        uint32_t bound = 1;  // (0 is no key)
+#pragma unroll
+        for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1)
+            if (const uint32_t to = (bound & ~1u) | bit; __popcll(__ballot(head >= to)) >= C.top_k) bound = to;
+        for (int i = threadIdx.x; i < n; i += T) {
+            const uint64_t key = all[i];
+            if ((uint32_t)(key >> 32) < bound) continue;
+            const int at = atomicAdd(&candidates, 1);  // (in any order: their places are their own)
+            if (at < kCandidates) keys[at / kWave][at % kWave] = key;
+        }
+        __syncthreads();
+        const int found = candidates;
+        const uint64_t* list = &keys[0][0];
+        if (found >= C.top_k && found <= kCandidates) {
+            if ((int)threadIdx.x >= found) return;
+            const uint64_t mine = list[threadIdx.x];
+            int place = 0;
+#pragma unroll 4
+            for (int i = 0; i < found; ++i) place += list[i] > mine;
+            store_likeliest(C, row, s, f.ln, mine, place);
+            return;
+        }
+        __syncthreads();
+        uint64_t mine = 0;
+        for (int i = wave; i < P.segments; i += T / kWave) mine = merge_keys(mine, lane < C.top_k ? all[(int64_t)i * C.top_k + lane] : 0, lane);
         mine = merge_waves<T>(mine, keys, lane, wave);
         if (wave == 0)
             store_likeliest(C, row, s, f.ln, fill<VT>(mine, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
     }
-    if (threadIdx.x == 0) store_results(C, row, f);
 }
 
 template <int VT, bool DISTILL>

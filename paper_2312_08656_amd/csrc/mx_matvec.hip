@@ -4,11 +4,11 @@
 //
 // One row of X (two of 4 or 2 bytes in more than one bf16 part): a lane has a block of 32 columns of X in registers and takes that block of one row of W after the other,
 // 16 bytes a load, 16 conversions and 32 multiply-adds; the lanes of a row are added up.  100003 rows of 4096 columns, bf16: 37.7 us (5.8 TB/s, what
-// stays in the Infinity Cache included; matrix instructions: 51); fp32 45.7 (95).
+// stays in the Infinity Cache included; matrix instructions: 50); fp32 45.7 (83).
 //
 // More rows: matrix instructions take W as it decodes, exact in bf16, and X in bf16 parts that add up to it (three of fp32, two of fp16), so that products are
 // exact, and 2 to 16 rows cost the same.  A wavefront has 16 TILES rows of W and 512 columns at a time; the wavefronts of a workgroup share out the columns and
-// are joined in LDS.  What the parts of X take of the vector units and X of the caches' bandwidth bounds 16 rows: 8192 x 8192, fp32 23 us, bf16 15 (W alone: 7).
+// are joined in LDS.  The cutting of X takes the vector units 10 us of 16 rows of fp32 by 8192 x 8192, 19 in all, bf16 12.6 (W alone: 7); 16 rows of bf16, 4096 to 100003, 59.
 #include "mx_parts.hpp"
 #include "rows.hpp"
 
@@ -42,14 +42,14 @@ __device__ __forceinline__ void x_parts(const float (&x)[kRowUnit], bf16x8 (&par
 // Rows of W and of X as a lane has them
 template <int VT, int TILES>
 struct Operands {
-    const uint8_t *code[TILES], *scale[TILES];  // its row of each tile
+    const uint8_t *code[TILES], *scale[TILES];  // its row of each tile as a matrix operand
+    const uint8_t* line[TILES];                 // its row and block as it reads memory
     const value_store_t<VT>*x, *x_end;
     int din, nb, quarter;
 };
 
 // A row's four lanes have a block each; after it each has a quarter of every one of the four: 8 columns, those of its place in the row's four lanes, so that
-// what a matrix instruction takes of X is 32 columns of a row side by side.  (Where each lane takes a block of X, an access is 16 bytes of 64 lines:
-// 16 rows of fp32, 4096 to 100003, 126 us instead of 108.)
+// what a matrix instruction takes of X is 32 columns of a row side by side.
 __device__ __forceinline__ void share_blocks(uint4& c)
 {
     const auto xz = __builtin_amdgcn_permlane32_swap(c.x, c.z, false, false), yw = __builtin_amdgcn_permlane32_swap(c.y, c.w, false, false);
@@ -71,10 +71,64 @@ __device__ __forceinline__ uint32_t four_scales(const uint8_t* s, int b, int nb)
     return w;
 }
 
+// 4 blocks (128 columns) of X and of W for a wavefront: four lanes have 64 bytes of a row side by side, as the caches want them, and write them to LDS, where the lanes read what
+// the matrix instruction takes of 16 rows.  (Read from memory in that order, neighbouring lanes have different rows, and an access is 64 of the
+// cache's instead of 16: 16 rows, 4096 to 100003, fp32 108 us, bf16 77.)
+// Pieces of 16 bytes lie in each fourth row at another place, so that rows fall on different banks.
+__device__ __forceinline__ int own_piece(int lane) { return (lane & 3) ^ (lane >> 4 & 3); }  // as memory is read: of row lane / 4
+__device__ __forceinline__ int piece_at(int row, int piece) { return row * 64 + (piece ^ (row >> 2 & 3)) * 16; }
+template <int VT>
+struct Staged {
+    static constexpr int kLoads = VT == MAXK_VALUE_F32 ? 8 : 4;      // of 1 KiB
+    static constexpr int kElements = VT == MAXK_VALUE_F32 ? 4 : 8;   // of 16 bytes
+    const value_store_t<VT>* x;  // this lane's row and piece as it reads memory
+    uint8_t* room;               // kLoads KiB, and one for each tile of W
+    int lane;
+    uint4 way[kLoads];
+
+    __device__ __forceinline__ void begin(const value_store_t<VT>* X, int64_t n0, int64_t N, int din, uint8_t* room_, int lane_)
+    {
+        lane = lane_, room = room_;
+        const int row = lane >> 2;
+        x = X + min(n0 + row, N - 1) * din + own_piece(lane) * kElements;  // (rows behind the last one of X: it again)
+    }
+    __device__ __forceinline__ void ask(int block)
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) way[j] = read16(x + block * kMxBlock + j * 4 * kElements);
+    }
+    template <int TILES>
+    __device__ __forceinline__ void put(uint4 (&code)[TILES][4], int i)  // and block i of each lane's codes, which come back for the other order
+    {
+        uint8_t* w = room + kLoads * 1024;
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) *reinterpret_cast<uint4*>(room + j * 1024 + lane * 16) = way[j];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) *reinterpret_cast<uint4*>(w + t * 1024 + lane * 16) = code[t][i];
+        wave_fence();
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) code[t][i] = *reinterpret_cast<const uint4*>(w + t * 1024 + piece_at(lane & 15, lane >> 4));
+    }
+    __device__ __forceinline__ uint4 piece(int i) const  // of 16 bytes of the lane's row as a matrix operand
+    {
+        return *reinterpret_cast<const uint4*>(room + (i >> 2) * 1024 + piece_at(lane & 15, i & 3));
+    }
+    __device__ __forceinline__ RawUnit<VT> get(int q) const  // the lane's 8 columns of block q
+    {
+        const int quarter = lane >> 4;
+        RawUnit<VT> u;
+        if constexpr (VT == MAXK_VALUE_F32) u.w[0] = piece(8 * q + 2 * quarter), u.w[1] = piece(8 * q + 2 * quarter + 1);
+        else u.w[0] = piece(4 * q + quarter);
+        return u;
+    }
+};
+
 // 16 blocks of columns from block b0 on (WHOLE: all of them lie in the rows)
 template <int VT, int TILES, bool WHOLE>
-__device__ __forceinline__ void multiply(const Operands<VT, TILES>& O, int b0, f32x4v (&sum)[TILES])
+__device__ __forceinline__ void multiply(const Operands<VT, TILES>& O, Staged<VT>& staged, int b0, f32x4v (&sum)[TILES])
 {
+    if constexpr (WHOLE) staged.ask(b0);
     uint4 code[TILES][4];
     uint32_t scale[TILES][4];
 #pragma unroll
@@ -88,7 +142,8 @@ __device__ __forceinline__ void multiply(const Operands<VT, TILES>& O, int b0, f
             const int b = b0 + i * 4 + O.quarter;
             if constexpr (!WHOLE) scale[t][i] = four_scales(O.scale[t], b0 + i * 4, O.nb);
             code[t][i] = make_uint4(0, 0, 0, 0);
-            if (WHOLE || b < O.nb) code[t][i] = *reinterpret_cast<const uint4*>(O.code[t] + b * 16);
+            if constexpr (WHOLE) code[t][i] = *reinterpret_cast<const uint4*>(O.line[t] + (b0 + i * 4) * 16);
+            else if (b < O.nb) code[t][i] = *reinterpret_cast<const uint4*>(O.code[t] + b * 16);
         }
     }
 #pragma unroll
@@ -96,10 +151,14 @@ __device__ __forceinline__ void multiply(const Operands<VT, TILES>& O, int b0, f
         if (!WHOLE && b0 + i * 4 >= O.nb) break;
         const int first = (b0 + i * 4) * kMxBlock + O.quarter * kRowUnit;
         RawUnit<VT> raw[4];
+        if constexpr (WHOLE) {
+            staged.put(code, i);
+            if (i < 3) staged.ask(b0 + (i + 1) * 4);
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int col = first + q * kMxBlock;
-            if constexpr (WHOLE) raw[q] = whole_unit<VT>(O.x + col);
+            if constexpr (WHOLE) raw[q] = staged.get(q);
             else raw[q] = fetch_row_unit<VT>(O.x + col, O.din - col, O.x_end);
         }
 #pragma unroll
@@ -131,11 +190,15 @@ __device__ __forceinline__ void multiply(const Operands<VT, TILES>& O, int b0, f
     }
 }
 
+template <int VT, int TILES> constexpr int matvec_room = (Staged<VT>::kLoads + TILES) * 1024;  // of a wavefront: what is staged, its sums in the end
+
 template <int VT, int TILES>
 __global__ void __launch_bounds__(kMostWaves* kWave) matvec_kernel(const value_store_t<VT>* X, int64_t N, const uint8_t* codes, const uint8_t* scales, int din,
                                                                    int dout, const float* bias, void* Y, int y_type)
 {
-    __shared__ f32x4v sums[kMostWaves][TILES][kWave];
+    extern __shared__ uint4 rooms[];  // of every wavefront
+    constexpr int kRoom = matvec_room<VT, TILES>;
+    uint8_t* room = reinterpret_cast<uint8_t*>(rooms);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     const int nb = mx_blocks(din), row16 = lane & 15, quarter = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.y * kRows, n = n0 + row16;
@@ -151,18 +214,21 @@ __global__ void __launch_bounds__(kMostWaves* kWave) matvec_kernel(const value_s
         const int64_t o = min(o0 + t * 16 + row16, (int64_t)dout - 1);
         O.code[t] = codes + o * nb * 16;
         O.scale[t] = scales + o * nb;
+        O.line[t] = codes + (min(o0 + t * 16 + (lane >> 2), (int64_t)dout - 1) * nb + own_piece(lane)) * 16;
     }
+    Staged<VT> staged;
+    staged.begin(X, n0, N, din, room + wave * kRoom, lane);
     for (int b0 = wave * kBlocks; b0 < nb; b0 += waves * kBlocks) {
-        if ((b0 + kBlocks) * kMxBlock <= din) multiply<VT, TILES, true>(O, b0, sum);
-        else multiply<VT, TILES, false>(O, b0, sum);
+        if ((b0 + kBlocks) * kMxBlock <= din) multiply<VT, TILES, true>(O, staged, b0, sum);
+        else multiply<VT, TILES, false>(O, staged, b0, sum);
     }
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) sums[wave][t][lane] = sum[t];
+    for (int t = 0; t < TILES; ++t) *reinterpret_cast<f32x4v*>(room + wave * kRoom + t * 1024 + lane * 16) = sum[t];
     __syncthreads();
     if (n >= N) return;
     for (int t = wave; t < TILES; t += waves) {
-        f32x4v y = sums[0][t][lane];
-        for (int w = 1; w < waves; ++w) y += sums[w][t][lane];
+        f32x4v y = *reinterpret_cast<const f32x4v*>(room + t * 1024 + lane * 16);
+        for (int w = 1; w < waves; ++w) y += *reinterpret_cast<const f32x4v*>(room + w * kRoom + t * 1024 + lane * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t o = o0 + t * 16 + quarter * 4 + j, at = n * dout + o;
@@ -178,7 +244,8 @@ __global__ void __launch_bounds__(kMostWaves* kWave) matvec_kernel(const value_s
 template <int VT, int TILES>
 maxk_status run_matvec(const void* X, int64_t N, const MxMatrix& W, int din, int dout, const float* bias, void* Y, int y_type, int waves, hipStream_t s)
 {
-    hipLaunchKernelGGL((matvec_kernel<VT, TILES>), dim3((unsigned)((dout + 16 * TILES - 1) / (16 * TILES)), (unsigned)((N + kRows - 1) / kRows)), dim3(waves * kWave), 0, s,
+    const unsigned room = (unsigned)waves * matvec_room<VT, TILES>;
+    hipLaunchKernelGGL((matvec_kernel<VT, TILES>), dim3((unsigned)((dout + 16 * TILES - 1) / (16 * TILES)), (unsigned)((N + kRows - 1) / kRows)), dim3(waves * kWave), room, s,
                        (const value_store_t<VT>*)X, N, W.codes, W.scales, din, dout, bias, Y, y_type);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
@@ -316,18 +383,16 @@ maxk_status matvec(const void* X, int64_t N, const MxMatrix& W, int din, int dou
 {
     if (mx_blocks(din) <= kMostLaneBlocks) {
         if (N == 1) return matvec_lanes<VT, 1>(X, W, din, dout, bias, Y, y_type, s);
-        // a second row costs the matrix instructions nothing but fp32's and fp16's parts: 100003 x 4096, two rows, lanes / matrix instructions 63 / 95 us fp32, 56 / 51 bf16
+        // a second row costs the matrix instructions nothing but fp32's and fp16's parts: 100003 x 4096, two rows, lanes / matrix instructions 63 / 83 us fp32, 56 / 50 bf16
         if constexpr (kParts<VT> > 1)
             if (N == 2) return matvec_lanes<VT, 2>(X, W, din, dout, bias, Y, y_type, s);
     }
-    const int shares = (mx_blocks(din) + kBlocks - 1) / kBlocks, waves = std::min(shares, kMostWaves);
-    // Tiles of 16 rows of W a wavefront: X is read and cut up once for all of them.  Two as long as there are workgroups for half of the CUs, four where
-    // there is enough for all of them several times.  us, 1 / 2 / 4 tiles, 16 rows: fp32 4096 x 4096 11.7 / 12.8 / 15.6, 8192 x 8192 35.8 / 23.2 / 29.0, 4096 to 100003
-    // 207 / 147 / 108; bf16 8192 x 8192 22.0 / 15.2 / 19.7, 4096 to 100003 125 / 90 / 77
-    const int groups = (dout + 15) / 16;
-    if (groups >= 4 * 1024) return run_matvec<VT, 4>(X, N, W, din, dout, bias, Y, y_type, waves, s);
-    if (groups >= 2 * 192) return run_matvec<VT, 2>(X, N, W, din, dout, bias, Y, y_type, waves, s);
-    return run_matvec<VT, 1>(X, N, W, din, dout, bias, Y, y_type, waves, s);
+    // Two tiles a wavefront, for which X is read and cut up once, where that leaves workgroups for three quarters of the CUs; four wavefronts with larger shares of
+    // the columns where there are four workgroups a CU and more.  us, 1 tile and 8 wavefronts / 2 and 8 / 2 and 4 / 4 and 4, 16 rows: fp32 4096 x 4096 9.3 / 10.1 / 11.4 /
+    // 16.5, 8192 x 8192 22.3 / 19.0 / 22.2 / 30.7, 4096 to 100003 137 / 124 / 92 / 90; bf16 8192 x 8192 13.9 / 12.6 / 14.8 / 19.6, 4096 to 100003 89 / 61 / 59 / 62
+    const int shares = (mx_blocks(din) + kBlocks - 1) / kBlocks, pairs = (dout + 31) / 32;
+    if (pairs < 192) return run_matvec<VT, 1>(X, N, W, din, dout, bias, Y, y_type, std::min(shares, kMostWaves), s);
+    return run_matvec<VT, 2>(X, N, W, din, dout, bias, Y, y_type, std::min(shares, pairs < 4 * 256 ? kMostWaves : kMostWaves / 2), s);
 }
 
 }  // namespace

@@ -50,6 +50,15 @@ def test_many_rows_of_weights(N):
         check(torch.from_numpy(mx_common.features(rng, N, 200)).cuda().to(dtype), codes, scales, W, None, dtype)
 
 
+@pytest.mark.parametrize("din,dout", [(1100, 33001), (9001, 6500), (4096, 6200), (2049, 32800)])
+def test_many_columns_and_rows(din, dout):
+    """Two tiles a wavefront, few and many wavefronts, several rounds of each, the last one whole and not."""
+    rng = np.random.default_rng(din)
+    codes, scales, W = weights(rng, dout, din)
+    for N, dtype in ((3, torch.float32), (16, torch.bfloat16), (5, torch.float16), (2, torch.bfloat16)):
+        check(torch.from_numpy(mx_common.features(rng, N, din)).cuda().to(dtype), codes, scales, W, None, dtype)
+
+
 def test_offsets_and_what_lies_around():
     rng = np.random.default_rng(4)
     N, din, dout = 3, 77, 45
