@@ -273,9 +273,24 @@ __device__ __forceinline__ uint64_t fill(uint64_t key, const value_store_t<VT>* 
 
 // ---- a row ----
 
-__device__ __forceinline__ int64_t label_of(const ClassCall& C, int64_t row)
+// What a row is asked for beside its logits.  (Loads without a branch on what they bring, and before anything waits: a short row's time is these.)
+struct Given {
+    int64_t y;         // the class, -1: none
+    float g, u;        // of the log probability, of the entropy; of the loss
+};
+__device__ __forceinline__ Given row_given(const ClassCall& C, int64_t row)
 {
-    return C.label_bytes == 8 ? ((const int64_t*)C.labels)[row] : (int64_t)((const int32_t*)C.labels)[row];
+    Given w = {-1, 0.f, 0.f};
+    int32_t low = -1, high = -1;
+    if (C.labels) {
+        const int32_t* p = (const int32_t*)C.labels + row * (C.label_bytes / 4);
+        low = p[0], high = p[C.label_bytes / 4 - 1];
+    }
+    if (C.dlogprob) w.g = C.dlogprob[row];
+    if (C.dloss) w.g = C.dloss[row];
+    if (C.dentropy) w.u = C.dentropy[row];
+    w.y = C.label_bytes == 8 ? (int64_t)((uint64_t)(uint32_t)high << 32 | (uint32_t)low) : (int64_t)low;
+    return w;
 }
 __device__ __forceinline__ int64_t column_of(const ClassCall& C, int64_t at)
 {
@@ -381,15 +396,14 @@ __device__ __forceinline__ void sum_of_column(const ClassCall& C, const Entries&
 }
 
 template <int VT>
-__device__ __forceinline__ Asked given_class(const ClassCall& C, int64_t row)
+__device__ __forceinline__ Asked given_class(const ClassCall& C, int64_t row, const Given& w)
 {
-    const int64_t y = C.labels ? label_of(C, row) : -1;
-    return {y >= 0 && y < C.V ? widen_value<VT>(((const value_store_t<VT>*)C.logits)[row * C.V + y]) : 0.f, 0.f, 0.f, 0.f};
+    return {w.y >= 0 && w.y < C.V ? widen_value<VT>(((const value_store_t<VT>*)C.logits)[row * C.V + w.y]) : 0.f, 0.f, 0.f, 0.f};
 }
 
 struct Found { float ln, logprob, entropy, loss; };  // of a whole row; ln = ln S
 
-__device__ __forceinline__ Found row_results(const ClassCall& C, int64_t row, const Sums& s, const Asked& a)
+__device__ __forceinline__ Found row_results(const ClassCall& C, const Given& w, const Sums& s, const Asked& a)
 {
     Found f = {logf(s.S), 0.f, 0.f, 0.f};
     if (C.index) {
@@ -397,8 +411,7 @@ __device__ __forceinline__ Found row_results(const ClassCall& C, int64_t row, co
         return f;
     }
     f.entropy = s.S == 0.f ? 0.f : f.ln - kLn2 * (s.T / s.S);
-    const int64_t y = C.labels ? label_of(C, row) : -1;
-    f.logprob = y < 0 ? 0.f : y >= C.V ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (a.x - s.m) - f.ln;
+    f.logprob = w.y < 0 ? 0.f : w.y >= C.V ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (a.x - s.m) - f.ln;
     return f;
 }
 
@@ -423,17 +436,16 @@ __device__ __forceinline__ void store_likeliest(const ClassCall& C, int64_t row,
 
 // dx = e (A + B d) + g at the given class
 struct Slope { float A, B, g; int64_t y; };
-__device__ __forceinline__ Slope row_slope(const ClassCall& C, int64_t row, const Sums& s, const Asked& a, const Found& f)
+__device__ __forceinline__ Slope row_slope(const ClassCall& C, const Given& w, const Sums& s, const Asked& a, const Found& f)
 {
     const float inverse = 1.f / s.S;
     if (C.index) {
-        const float g = C.dloss[row] * C.scale;
+        const float g = w.g * C.scale;
         return {s.S == 0.f ? 0.f : g * a.Q * inverse, 0.f, s.S == 0.f ? 0.f : g, -1};
     }
-    const int64_t y = C.labels ? label_of(C, row) : -1;
-    const float g = !C.dlogprob || y < 0 ? 0.f : y >= C.V ? __builtin_nanf("") : C.dlogprob[row], u = C.dentropy ? C.dentropy[row] : 0.f;
+    const float g = !C.dlogprob || w.y < 0 ? 0.f : w.y >= C.V ? __builtin_nanf("") : w.g, u = w.u;
     if (s.S == 0.f) return {g != g ? g : 0.f, 0.f, 0.f, -1};
-    return {(-g + u * (f.ln - f.entropy)) * inverse, -u * kLn2 * inverse, g, y};
+    return {(-g + u * (f.ln - f.entropy)) * inverse, -u * kLn2 * inverse, g, w.y};
 }
 
 // Columns from `first` on up to the next line of 128 bytes in memory (fewer: up to `last`)
@@ -884,7 +896,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     float* mine = spread + (DISTILL && GRAD ? team * L * U * kRowUnit : 0);
     Asked asked;
     std::conditional_t<DISTILL, TeamEntries<VT, L, U, GRAD>, Nothing> entries(C, row, lane, mine);
-    if constexpr (!DISTILL) asked = given_class<VT>(C, row);
+    const Given given = row_given(C, row);
     float v[U][kRowUnit];
 #pragma unroll
     for (int u = 0; u < U; ++u) unit_values<VT>(raw[u], C.V - (lane + u * L) * kRowUnit, -__builtin_inff(), v[u]);
@@ -905,8 +917,17 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         }
     s.S = over_lanes<L>(s.S, kAdd);
     if constexpr (!DISTILL) s.T = over_lanes<L>(s.T, kAdd);
-    if constexpr (DISTILL) asked = entries.take();
-    const Found f = row_results(C, row, s, asked);
+    if constexpr (DISTILL) {
+        asked = entries.take();
+    } else {
+        float x_given = 0.f;  // of the lane that has the class
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j) x_given = given.y == (lane + u * L) * kRowUnit + j ? v[u][j] : x_given;
+        asked = {over_lanes<L>(x_given, kAdd), 0.f, 0.f, 0.f};
+    }
+    const Found f = row_results(C, given, s, asked);
     if (lane == 0) store_results(C, row, f);
     if constexpr (TOP && L == kWave) {
         Likeliest best;
@@ -926,7 +947,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         else likeliest_by_place<L>(C, row, s, f.ln, v[0], lane, places + team * L * kRowUnit);
     }
     if constexpr (GRAD) {
-        const Slope k = row_slope(C, row, s, asked, f);
+        const Slope k = row_slope(C, given, s, asked, f);
         S* dx = (S*)C.dlogits + row * C.V;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -972,7 +993,7 @@ __global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
         const int64_t r = row0 + i * kBring + threadIdx.x / 8;
         raw[i] = fetch_row_unit<VT>(x + r * C.V + part, r < C.N ? C.V - part : 0, end);
     }
-    const Asked asked = given_class<VT>(C, min(row, C.N - 1));
+    const Given given = row_given(C, min(row, C.N - 1));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float* to = rows_of_lanes + (i * kBring + threadIdx.x / 8) * pitch + part;
@@ -1021,6 +1042,7 @@ __global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
             for (int i = 0; i < K; ++i) best[i] = unpaired(whole[i]);
         }
     }
+    const Asked asked = {given.y >= 0 && given.y < C.V ? mine[given.y] : 0.f, 0.f, 0.f, 0.f};
     Sums s = no_sums();
     s.m = fmaxf(key_value((uint32_t)(best[0] >> 32)), s.m);  // (a NaN, which is greater than all others, makes S one)
 #pragma unroll 4
@@ -1029,7 +1051,7 @@ __global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
         s.S += e;
         s.T = fmaf(e, fmaxf(d, -kFar), s.T);
     }
-    const Found f = row_results(C, row, s, asked);
+    const Found f = row_results(C, given, s, asked);
     store_results(C, row, f);
 #pragma unroll
     for (int i = 0; i < K; ++i)
@@ -1057,12 +1079,13 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
             else asked = take_more_entries<VT>(C, row, lane, entries);
             if (lane == 0) asked_room = asked;
         }
-    } else {
-        asked = given_class<VT>(C, row);
     }
-    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, 0, C.V, best, room, kNothing);
+    const Given given = row_given(C, row);
+    const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, 0, C.V, best, room, [&] {
+        if constexpr (!DISTILL) asked = given_class<VT>(C, row, given);
+    });
     if constexpr (DISTILL) asked = asked_room;
-    const Found f = row_results(C, row, s, asked);
+    const Found f = row_results(C, given, s, asked);
     if constexpr (TOP) {
         best.end();
         const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
@@ -1071,7 +1094,7 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     }
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (GRAD) {
-        const Slope k = row_slope(C, row, s, asked, f);
+        const Slope k = row_slope(C, given, s, asked, f);
         if constexpr (DISTILL) store_gradient<VT, T, true>(C, row, 0, C.V, s, k, &entries, kNothing);
         else store_gradient<VT, T, false>(C, row, 0, C.V, s, k, nullptr, kNothing);
     }
@@ -1101,13 +1124,15 @@ __global__ void __launch_bounds__(kThreads) class_parts_kernel(ClassCall C, Part
     const bool asks = segment == 0 && wave == 0;
     Asked asked;
     FewEntries<VT> few;
+    Given given;
     if (asks) {
-        if constexpr (!DISTILL) asked = given_class<VT>(C, row);
+        if constexpr (!DISTILL) given = row_given(C, row);
         else if (C.k <= kFewEntries) few.ask(C, row, lane);
     }
     const Sums s = sum_row<VT, T, !DISTILL, TOP>(C, row, first, last, best, room, [&] {
         if (!asks) return;
         if constexpr (DISTILL) asked = C.k <= kFewEntries ? few.take(C, lane, false, entries) : take_more_entries<VT>(C, row, lane, entries);
+        else asked = given_class<VT>(C, row, given);
         if (lane == 0) P.asked[row] = asked;
     });
     if (threadIdx.x == 0) P.sums[blockIdx.x] = s;
@@ -1142,7 +1167,7 @@ __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
         if (threadIdx.x == 0) candidates = 0;
     }
     const Sums s = join_segments<T>(C, P, row, sums_room);
-    const Found f = row_results(C, row, s, P.asked[row]);
+    const Found f = row_results(C, row_given(C, row), s, P.asked[row]);
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (TOP) {
         const uint64_t* all = P.keys + row * P.segments * C.top_k;
@@ -1198,9 +1223,10 @@ __global__ void __launch_bounds__(kThreads) class_gradient_kernel(ClassCall C, P
     }
     const Sums s = join_segments<T>(C, P, row, room);
     const Asked asked = P.asked[row];
-    const Found f = row_results(C, row, s, asked);
+    const Given given = row_given(C, row);
+    const Found f = row_results(C, given, s, asked);
     if (segment == 0 && threadIdx.x == 0) store_results(C, row, f);
-    const Slope k = row_slope(C, row, s, asked, f);
+    const Slope k = row_slope(C, given, s, asked, f);
     if constexpr (DISTILL)
         store_gradient<VT, T, true>(C, row, first, last, s, k, &entries, [&] {
             if (threadIdx.x < kWave && C.k <= kFewEntries) few.take(C, threadIdx.x, true, entries);
