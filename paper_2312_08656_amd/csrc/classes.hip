@@ -252,12 +252,13 @@ struct Likeliest {
     __device__ __forceinline__ void end() { while (waiting > 0) sort_in(); }
 };
 
-// The keys of a row in falling order, filled up to k with its first masked columns where there are fewer.  (room: k keys in LDS of the wavefront)
+// The keys of a row in falling order, filled up to k with its first masked columns where there are fewer.  (room: k keys in LDS of the wavefront.  A row with a NaN,
+// whose S is one, has no order, and might be gone through to its end.)
 template <int VT>
-__device__ __forceinline__ uint64_t fill(uint64_t key, const value_store_t<VT>* x, int V, int k, int lane, uint64_t* room)
+__device__ __forceinline__ uint64_t fill(uint64_t key, const Sums& s, const value_store_t<VT>* x, int V, int k, int lane, uint64_t* room)
 {
     int have = __popcll(__ballot(lane < k && key));
-    if (have >= k) return key;
+    if (have >= k || s.S != s.S) return key;
     const int found = have;
     for (int base = 0; base < V && have < k; base += kWave) {
         const int col = base + lane;
@@ -272,6 +273,11 @@ __device__ __forceinline__ uint64_t fill(uint64_t key, const value_store_t<VT>* 
 }
 
 // ---- a row ----
+
+// Workgroups in two dimensions: in one the threads of a launch have to be fewer than 2^32
+constexpr int64_t kMostGroupsAcross = 1 << 20;
+dim3 groups_of(int64_t n) { return dim3((unsigned)std::min(n, kMostGroupsAcross), (unsigned)((n + kMostGroupsAcross - 1) / kMostGroupsAcross)); }
+__device__ __forceinline__ int64_t group_number() { return (int64_t)blockIdx.y * kMostGroupsAcross + blockIdx.x; }
 
 // What a row is asked for beside its logits.  (Loads without a branch on what they bring, and before anything waits: a short row's time is these.)
 struct Given {
@@ -883,7 +889,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? kWaiting : 1];
     __shared__ __attribute__((aligned(16))) uint32_t places[TOP && L < kWave ? kThreads * kRowUnit : 1];
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
-    const int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    const int64_t row = group_number() * kTeams + team;
     if (row >= C.N) return;
     const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
     const float c = C.scale * kLog2e;
@@ -939,7 +945,7 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
             best.offer(v[u], largest(v[u]), col, C.V - col);
         }
         best.end();
-        store_likeliest(C, row, s, f.ln, fill<VT>(best.mine, x, C.V, C.top_k, lane, keys[team]), lane);
+        store_likeliest(C, row, s, f.ln, fill<VT>(best.mine, s, x, C.V, C.top_k, lane, keys[team]), lane);
     } else if constexpr (TOP) {
         static_assert(U == 1);
         // Few alternatives in rounds, some fifty instructions each; many by their places, 18 instructions a column.  us, 27685 rows of 41 bf16 with all of them, 21 / 12
@@ -985,7 +991,8 @@ __global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
     constexpr int kBring = kThreads / 8;  // rows an access
     extern __shared__ float rows_of_lanes[];
     const int pitch = lane_row_pitch(C.V), part = threadIdx.x % 8 * kRowUnit;
-    const int64_t row0 = (int64_t)blockIdx.x * kThreads, row = row0 + threadIdx.x;
+    const int64_t row0 = group_number() * kThreads, row = row0 + threadIdx.x;
+    if (row0 >= C.N) return;
     const S *x = (const S*)C.logits, *end = x + C.N * C.V;
     RawUnit<VT> raw[8];
 #pragma unroll
@@ -1067,7 +1074,8 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
     __shared__ Asked asked_room;
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     __shared__ uint64_t keys[TOP ? T / kWave : 1][kWaiting];
-    const int64_t row = blockIdx.x;
+    const int64_t row = group_number();
+    if (row >= C.N) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
     Likeliest best;
     if constexpr (TOP) best.begin(C.top_k, keys[wave], lane);
@@ -1090,7 +1098,7 @@ __global__ void __launch_bounds__(T, TOP ? 4 : 8) class_rows_kernel(ClassCall C)
         best.end();
         const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
         if (wave == 0)
-            store_likeliest(C, row, s, f.ln, fill<VT>(key, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
+            store_likeliest(C, row, s, f.ln, fill<VT>(key, s, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
     }
     if (threadIdx.x == 0) store_results(C, row, f);
     if constexpr (GRAD) {
@@ -1201,7 +1209,7 @@ __global__ void __launch_bounds__(T) class_join_kernel(ClassCall C, Parts P)
         for (int i = wave; i < P.segments; i += T / kWave) mine = merge_keys(mine, lane < C.top_k ? all[(int64_t)i * C.top_k + lane] : 0, lane);
         mine = merge_waves<T>(mine, keys, lane, wave);
         if (wave == 0)
-            store_likeliest(C, row, s, f.ln, fill<VT>(mine, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
+            store_likeliest(C, row, s, f.ln, fill<VT>(mine, s, (const value_store_t<VT>*)C.logits + row * C.V, C.V, C.top_k, lane, keys[0]), lane);
     }
 }
 
@@ -1261,7 +1269,7 @@ template <int VT, int L, int U, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_teams(const ClassCall& C, hipStream_t s)
 {
     constexpr int kTeams = kThreads / L;
-    hipLaunchKernelGGL((class_team_kernel<VT, L, U, DISTILL, GRAD, TOP>), dim3((unsigned)((C.N + kTeams - 1) / kTeams)), dim3(kThreads), 0, s, C);
+    hipLaunchKernelGGL((class_team_kernel<VT, L, U, DISTILL, GRAD, TOP>), groups_of((C.N + kTeams - 1) / kTeams), dim3(kThreads), 0, s, C);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
@@ -1269,7 +1277,7 @@ maxk_status run_teams(const ClassCall& C, hipStream_t s)
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_rows(const ClassCall& C, hipStream_t s)
 {
-    hipLaunchKernelGGL((class_rows_kernel<VT, T, DISTILL, GRAD, TOP>), dim3((unsigned)C.N), dim3(T), 0, s, C);
+    hipLaunchKernelGGL((class_rows_kernel<VT, T, DISTILL, GRAD, TOP>), groups_of(C.N), dim3(T), 0, s, C);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
@@ -1280,7 +1288,7 @@ constexpr int kManyRows = 2 * 256 * kThreads;
 template <int VT, int K>
 maxk_status run_lane_rows(const ClassCall& C, hipStream_t s)
 {
-    hipLaunchKernelGGL((class_lane_kernel<VT, K>), dim3((unsigned)((C.N + kThreads - 1) / kThreads)), dim3(kThreads), kThreads * lane_row_pitch(C.V) * sizeof(float), s, C);
+    hipLaunchKernelGGL((class_lane_kernel<VT, K>), groups_of((C.N + kThreads - 1) / kThreads), dim3(kThreads), kThreads * lane_row_pitch(C.V) * sizeof(float), s, C);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }

@@ -253,6 +253,8 @@ maxk_status run_matvec(const void* X, int64_t N, const MxMatrix& W, int din, int
 
 // ---- one row of X, or two: no matrix instructions ----
 
+constexpr int kMostGroupsAcross = 1 << 20;  // (in one dimension the threads of a launch have to be fewer than 2^32)
+
 // LANES lanes (a block of columns each) and COLS wavefronts share a row of W; a wavefront has BATCH of its rows, or 64 / LANES times as many, under way.
 template <int LANES, int COLS>
 struct LaneForm {
@@ -270,7 +272,7 @@ __global__ void __launch_bounds__((LaneForm<LANES, COLS>::kThreads))
     __shared__ float sums[COLS > 1 ? F::kWaves : 1][N][F::kStep];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave, part = wave % COLS, group = wave / COLS;
     const int nb = mx_blocks(din), b = part * LANES + lane % LANES;
-    const int64_t o0 = (int64_t)blockIdx.x * F::kRows + group * F::kStep;
+    const int64_t o0 = ((int64_t)blockIdx.y * kMostGroupsAcross + blockIdx.x) * F::kRows + group * F::kStep;
     uint4 code[F::kBatch];
     uint32_t scale[F::kBatch];
 #pragma unroll
@@ -356,7 +358,9 @@ template <int VT, int N, int LANES, int COLS>
 maxk_status run_lanes(const void* X, const MxMatrix& W, int din, int dout, const float* bias, void* Y, int y_type, hipStream_t s)
 {
     using F = LaneForm<LANES, COLS>;
-    hipLaunchKernelGGL((matvec_lanes_kernel<VT, N, LANES, COLS>), dim3((unsigned)((dout + F::kRows - 1) / F::kRows)), dim3(F::kThreads), 0, s,
+    const int groups = (dout + F::kRows - 1) / F::kRows;
+    const dim3 grid((unsigned)std::min(groups, kMostGroupsAcross), (unsigned)((groups + kMostGroupsAcross - 1) / kMostGroupsAcross));
+    hipLaunchKernelGGL((matvec_lanes_kernel<VT, N, LANES, COLS>), grid, dim3(F::kThreads), 0, s,
                        (const value_store_t<VT>*)X, W.codes, W.scales, din, dout, bias, Y, y_type);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;

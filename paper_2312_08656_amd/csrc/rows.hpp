@@ -54,14 +54,6 @@ __device__ __forceinline__ RawUnit<VT> whole_unit(const value_store_t<VT>* p)
     return u;
 }
 template <int VT>
-__device__ __forceinline__ void load_whole_unit(const value_store_t<VT>* p, float (&x)[kRowUnit])
-{
-    const RawUnit<VT> u = whole_unit<VT>(p);
-#pragma unroll
-    for (int j = 0; j < kRowUnit; ++j) x[j] = raw_value<VT>(u, j);
-}
-
-template <int VT>
 __device__ __forceinline__ void store_whole_unit(value_store_t<VT>* p, const float (&x)[kRowUnit])
 {
     value_store_t<VT> v[kRowUnit];

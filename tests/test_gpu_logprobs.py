@@ -117,6 +117,26 @@ def test_alternatives_of_many_short_rows(V, k, dtype):
         assert torch.isnan(data[400:402]).all() and torch.isnan(entropy[400:402]).all() and ((index[400:402] >= 0) & (index[400:402] < V)).all()
 
 
+@pytest.mark.parametrize("N,V", [(5, 20), (5, 60), (5, 250), (9, 500), (9, 2000), (9, 2500), (700, 5000), (600, 20001), (3, 16384), (5, 40000), (1, 200003)])
+def test_fewer_left_than_alternatives(N, V):
+    """0 to 30 columns of a row are not masked, of 20 and 64 alternatives: the first masked columns follow."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.full((N, V), -INF, device="cuda")
+        for n in range(0, N, max(1, N // 9)):
+            left = min((n * 7) % 31, V - 1) if n else 0
+            x[n, torch.randperm(V, generator=gen, device="cuda")[:left]] = torch.randn(left, generator=gen, device="cuda")
+        some = torch.arange(0, N, max(1, N // 9), device="cuda")
+        for k in (20, min(V, 64)):
+            _, _, data, index = results(N, k)
+            maxk.maxk_logprobs(x.to(dtype), None, None, None, data, index)
+            want = hc.likeliest(x.to(dtype)[some], k)
+            assert np.array_equal(index[some].cpu().numpy(), want)
+            left = torch.isfinite(torch.gather(x[some], 1, torch.from_numpy(want).cuda()))
+            assert torch.equal(torch.isfinite(data[some]), left) and (data[some][~left] == -INF).all()
+            assert N < 10 or (data[1] == -INF).all() and index[1].tolist() == list(range(k))
+
+
 def test_masks_of_the_lowest_value_and_of_everything():
     lowest = torch.finfo(torch.float32).min
     x = torch.full((4, 100), lowest, device="cuda")
@@ -135,6 +155,23 @@ def test_masks_of_the_lowest_value_and_of_everything():
     dx = torch.full_like(x, 7)
     maxk.maxk_logprobs_grad(x, dx, labels, torch.ones(4, device="cuda"), torch.ones(4, device="cuda"))
     assert torch.isfinite(dx).all() and (dx[2:] == 0).all() and abs(dx[0, 3].item() - 0.99) < 1e-6 and dx[1].abs().max() == 0
+
+
+@pytest.mark.parametrize("V", [16384, 50021])
+def test_non_finite_rows_in_segments(V):
+    x = torch.full((4, V), NAN, device="cuda")
+    x[1, : V - 1] = -INF
+    x[2, 1:] = 0.0
+    x[3, :] = 0.0
+    x[3, V - 1] = INF
+    _, _, data, index = results(4, 64)
+    logprob, entropy, dx = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros_like(x)
+    labels = torch.tensor([0, 1, -1, 3], device="cuda")
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    assert torch.isnan(logprob[[0, 1, 3]]).all() and logprob[2] == 0 and torch.isnan(entropy).all() and torch.isnan(data).all()
+    assert ((index >= 0) & (index < V)).all()
+    maxk.maxk_logprobs_grad(x, dx, labels, torch.ones(4, device="cuda"))
+    assert torch.isnan(dx[[0, 1, 3]]).all()
 
 
 @pytest.mark.parametrize("V", [47, 300, 1500, 9000])
@@ -227,6 +264,19 @@ def test_rows_past_32_bits():
     rows = torch.arange(N, device="cuda")
     assert ((x[rows, labels].float() - (1 - p)).abs() <= 2.0 ** -8 * (1 - p) + 1e-5).all()
     assert ((x[:, -1].float() + 1 / S).abs() <= 2.0 ** -8 / S + 1e-9).all()
+
+
+def test_as_many_rows_as_fit_no_launch_of_one_dimension():
+    """Four lanes a row: 2^30 rows are 2^32 threads."""
+    N = (1 << 30) + 12_345
+    x = torch.zeros(N, 1, dtype=torch.bfloat16, device="cuda")
+    entropy = torch.full((N,), 7.0, device="cuda")
+    logprob = torch.full((N,), 7.0, device="cuda")
+    labels = torch.zeros(N, dtype=torch.int32, device="cuda")
+    x[N - 2] = -INF
+    labels[N - 1] = 1
+    maxk.maxk_logprobs(x, labels, logprob, entropy)
+    assert not entropy.any().item() and torch.isnan(logprob[N - 1]) and logprob[N - 2] == -INF and not logprob[: N - 2].any().item()
 
 
 def test_no_rows():
