@@ -1065,6 +1065,115 @@ __global__ void __launch_bounds__(kThreads) class_lane_kernel(ClassCall C)
         if (i < C.top_k) store_likeliest(C, row, s, f.ln, best[i], i);
 }
 
+// ---- few classes of many rows, without alternatives: a lane a row ----
+
+// The rows of a workgroup are one stretch of memory, which goes to LDS and back 16 bytes an access whatever a row's length, and every lane has one of them
+// there, as it is stored, for itself: sums over a row pass no lane.  Where a row is an even number of words one more lies behind it, so that lanes are on different banks.
+struct Stretch {
+    int row;           // bytes of a row, of up to 64 elements and 8 at least
+    int words;         // of a row with one more behind it, 0: rows lie side by side
+    uint32_t inverse;  // of words
+
+    __host__ __device__ static Stretch of(int n, int size)
+    {
+        Stretch s = {n * size, 0, 0};
+        if (s.row % 8 == 0 && s.row >= 16) s.words = s.row / 4, s.inverse = (uint32_t)(((1ull << 32) + s.words - 1) / s.words);  // (exact: words there are fewer than 2^15)
+        return s;
+    }
+    __host__ __device__ int pitch() const { return words ? row + 4 : row; }
+    __host__ __device__ int room() const { return (kThreads * pitch() + 15) / 16 * 16; }
+    __device__ __forceinline__ int place(int byte) const { return words ? byte + 4 * (int)__umulhi((uint32_t)byte / 4, inverse) : byte; }
+    // a piece of 16 bytes: of at most two rows where a row is four words and more
+    template <typename F>
+    __device__ __forceinline__ void in_words(int piece, F&& word) const
+    {
+        const int first = piece * 4, number = (int)__umulhi((uint32_t)first, inverse), next = (number + 1) * words;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) word(i, first + i + number + (first + i >= next));
+    }
+    __device__ __forceinline__ void put(char* room, int piece, uint4 v) const
+    {
+        if (!words) {
+            *reinterpret_cast<uint4*>(room + piece * 16) = v;
+            return;
+        }
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        in_words(piece, [&](int i, int at) { reinterpret_cast<uint32_t*>(room)[at] = w[i]; });
+    }
+    __device__ __forceinline__ uint4 get(const char* room, int piece) const
+    {
+        if (!words) return *reinterpret_cast<const uint4*>(room + piece * 16);
+        uint32_t w[4];
+        in_words(piece, [&](int i, int at) { w[i] = reinterpret_cast<const uint32_t*>(room)[at]; });
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // `bytes` of memory to LDS, PIECES of 16 a lane under way at a time
+    template <int PIECES>
+    __device__ __forceinline__ void bring(const char* from, int bytes, char* room) const
+    {
+        const int pieces = bytes / 16;
+        for (int base = threadIdx.x; base < pieces; base += PIECES * kThreads) {
+            uint4 v[PIECES];
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (base + i * kThreads < pieces) v[i] = read16(from + (int64_t)(base + i * kThreads) * 16);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (base + i * kThreads < pieces) put(room, base + i * kThreads, v[i]);
+        }
+        if (const int at = pieces * 16 + threadIdx.x; at < bytes) room[place(at)] = from[at];
+    }
+    __device__ __forceinline__ void take(const char* room, int bytes, char* to) const
+    {
+        const int pieces = bytes / 16;
+        for (int piece = threadIdx.x; piece < pieces; piece += kThreads) write16(to + (int64_t)piece * 16, get(room, piece));
+        if (const int at = pieces * 16 + threadIdx.x; at < bytes) to[at] = room[place(at)];
+    }
+};
+constexpr int kLaneRowLeast = 8;  // (four words a row and more: in_words)
+template <int VT, bool GRAD, bool ENTROPY>
+__global__ void __launch_bounds__(kThreads) class_own_kernel(ClassCall C, Stretch R)
+{
+    using S = value_store_t<VT>;
+    extern __shared__ uint4 rooms_of_rows[];
+    char* const rows = reinterpret_cast<char*>(rooms_of_rows);
+    const int64_t row0 = group_number() * kThreads, row = row0 + threadIdx.x;
+    if (row0 >= C.N) return;
+    const int bytes = (int)min(C.N - row0, (int64_t)kThreads) * R.row;
+    R.bring<sizeof(S) * kLaneRowMost / 16>((const char*)C.logits + row0 * R.row, bytes, rows);
+    const Given given = row_given(C, min(row, C.N - 1));
+    __syncthreads();
+    if (row < C.N) {
+        S* const mine = reinterpret_cast<S*>(rows + threadIdx.x * R.pitch());
+        const float c = C.scale * kLog2e;
+        Sums s = no_sums();
+#pragma unroll 8
+        for (int j = 0; j < C.V; ++j) s.m = fmaxf(s.m, widen_value<VT>(mine[j]));
+#pragma unroll 8
+        for (int j = 0; j < C.V; ++j) {
+            const float d = (widen_value<VT>(mine[j]) - s.m) * c, e = exp2_of(d);
+            s.S += e;
+            if constexpr (ENTROPY) s.T = fmaf(e, fmaxf(d, -kFar), s.T);
+        }
+        const Asked asked = {given.y >= 0 && given.y < C.V ? widen_value<VT>(mine[given.y]) : 0.f, 0.f, 0.f, 0.f};
+        const Found f = row_results(C, given, s, asked);
+        store_results(C, row, f);
+        if constexpr (GRAD) {
+            const Slope k = row_slope(C, given, s, asked, f);
+            const int y = k.y < C.V ? (int)k.y : -1;
+#pragma unroll 8
+            for (int j = 0; j < C.V; ++j) {
+                const float d = (widen_value<VT>(mine[j]) - s.m) * c;
+                mine[j] = round_value<VT>(fmaf(exp2_of(d), ENTROPY ? fmaf(k.B, fmaxf(d, -kFar), k.A) : k.A, y == j ? k.g : 0.f));
+            }
+        }
+    }
+    if constexpr (GRAD) {
+        __syncthreads();
+        R.take(rows, bytes, (char*)C.dlogits + row0 * R.row);
+    }
+}
+
 // ---- a workgroup a row ----
 
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
@@ -1293,6 +1402,20 @@ maxk_status run_lane_rows(const ClassCall& C, hipStream_t s)
     return MAXK_OK;
 }
 
+// Where rows leave a quarter and more of a team's columns idle and there are many of them.  us, a lane a row / a team, 2.45 M rows, log probabilities and gradient:
+// 9 bf16 32 / 60, 17 48 / 60, 33 87 / 118, 47 123 / 139 (alone, without a gradient, 59 / 83), 47 fp32 184 / 240; 32 bf16 87 / 64, 56 143 / 127, 64 162 / 130; 600 k rows: 9 11 / 18,
+// 33 27 / 32, 41 33 / 33; 170 k: 47 16 / 13
+constexpr int kManyOwnRows = 1 << 19;
+bool own_rows(int64_t N, int V) { return N >= kManyOwnRows && V >= kLaneRowLeast && 4 * V < 3 * (V <= 4 * kRowUnit ? 4 : 8) * kRowUnit; }
+template <int VT, bool GRAD, bool ENTROPY>
+maxk_status run_own_rows(const ClassCall& C, hipStream_t s)
+{
+    const Stretch R = Stretch::of(C.V, sizeof(value_store_t<VT>));
+    hipLaunchKernelGGL((class_own_kernel<VT, GRAD, ENTROPY>), groups_of((C.N + kThreads - 1) / kThreads), dim3(kThreads), R.room(), s, C, R);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
 template <int VT, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
 {
@@ -1303,6 +1426,9 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
             if (keys <= 6) return run_lane_rows<VT, 6>(C, s);
             return run_lane_rows<VT, kLaneRowKeys>(C, s);
         }
+    if constexpr (!TOP && !DISTILL)
+        if (own_rows(C.N, C.V))
+            return C.entropy || C.dentropy ? run_own_rows<VT, GRAD, true>(C, s) : run_own_rows<VT, GRAD, false>(C, s);
     const int units = (C.V + kRowUnit - 1) / kRowUnit;
     if (units <= 4) return run_teams<VT, 4, 1, DISTILL, GRAD, TOP>(C, s);
     if (units <= 8) return run_teams<VT, 8, 1, DISTILL, GRAD, TOP>(C, s);

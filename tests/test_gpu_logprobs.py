@@ -137,6 +137,44 @@ def test_fewer_left_than_alternatives(N, V):
             assert N < 10 or (data[1] == -INF).all() and index[1].tolist() == list(range(k))
 
 
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("V", [8, 9, 16, 17, 23, 33, 40, 47])
+def test_many_short_rows(V, dtype):
+    """Rows enough for the form that has them in LDS as one stretch (a last one that is not full, rows of an even and an odd number of words, any element's alignment)."""
+    N = (1 << 19) + 225
+    x, labels, gen = inputs(N, V, dtype, V)
+    x[100:150] = torch.finfo(dtype).min
+    labels[150] = V
+    g, u = (torch.randn(N, generator=gen, device="cuda") for _ in range(2))
+    g[labels < 0] = 1.0
+    some = torch.cat([torch.arange(150), torch.arange(N - 300, N)]).cuda()
+    lp, lp_bound, H, H_bound, R = hc.logprobs(x[some], labels[some])
+    for dlogprob, dentropy, entropies in ((g, u, True), (g, None, True), (g, None, False), (None, u, False)):
+        dx = torch.full_like(x, 7)
+        logprob, entropy, _, _ = results(N)
+        maxk.maxk_logprobs_grad(x, dx, labels, dlogprob, dentropy, logprob=logprob, entropy=entropy if entropies else None)
+        hc.close(logprob[some], lp, lp_bound)
+        if entropies:
+            hc.close(entropy[some], H, H_bound)
+        pick = [None if t is None else t[some] for t in (dlogprob, dentropy)]
+        want, bound = hc.logprobs_grad(R, labels[some], *pick)
+        hc.close(dx[some], want, bound, dtype)
+        assert torch.isnan(logprob[150]) and (dlogprob is None or torch.isnan(dx[150]).all())
+    logprob2, entropy2, _, _ = results(N)
+    maxk.maxk_logprobs(x, labels.int(), logprob2, entropy2)
+    assert torch.equal(logprob2[151:], logprob[151:]) and torch.isnan(logprob2[150])
+    hc.close(entropy2[some], H, H_bound)
+    flat, out = (torch.full((N * V + 16,), 3.0, dtype=dtype, device="cuda") for _ in range(2))
+    for at, to in ((1, 2), (3, 0)):
+        flat[at:at + N * V].copy_(x.view(-1))
+        own = out[to:to + N * V].view(N, V)
+        maxk.maxk_logprobs_grad(flat[at:at + N * V].view(N, V), own, labels, None, u)
+        assert torch.equal(own, dx) and (out[:to] == 3).all() and (out[to + N * V:] == 3).all()
+        out[:] = 3
+    maxk.maxk_logprobs_grad(x, x, labels, None, u)  # in the logits' own memory
+    assert torch.equal(x, dx)
+
+
 def test_masks_of_the_lowest_value_and_of_everything():
     lowest = torch.finfo(torch.float32).min
     x = torch.full((4, 100), lowest, device="cuda")
