@@ -4,8 +4,8 @@
 //   log probabilities:  dx = p (-g - u (log p + H)), + g at the given class
 //   distillation:       q = softmax(scale t) of the teacher's entries;  loss = sum q (log q - log p);  dx = g scale (p - sum of q at the column)
 //
-// Rows of up to 2048 columns lie in the registers of a part of a wavefront or of all of it and are read once.  One pass over a longer row has its maximum and
-// sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end; the gradient reads the row again, from the caches, and
+// Rows of up to 2048 columns lie in the registers of a part of a wavefront or of all of it, of up to 16384 in a workgroup's, and are read once.  One pass over a longer row
+// has its maximum and sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end; the gradient reads the row again, from the caches, and
 // writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.
 #include "heads.hpp"
 #include "mx_parts.hpp"
@@ -1174,6 +1174,118 @@ __global__ void __launch_bounds__(kThreads) class_own_kernel(ClassCall C, Stretc
     }
 }
 
+// ---- a row in the registers of a workgroup ----
+
+// U units of 8 columns a thread: the maximum is known before the first exponential, so that wavefronts add up sums instead of joining them (six steps of two
+// exponentials each, which cost a wavefront as much as its columns in rows of 4000).
+template <int T, typename F>
+__device__ __forceinline__ float over_workgroup(float x, F&& f, float* room)  // (passes a barrier, room is free behind the next one)
+{
+    x = over_lanes<kWave>(x, f);
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = x;
+    __syncthreads();
+    return over_lanes<T / kWave>(room[threadIdx.x % (T / kWave)], f);
+}
+
+template <int VT, int T, int U, bool DISTILL, bool GRAD, bool TOP>
+__global__ void __launch_bounds__(T) class_held_kernel(ClassCall C)
+{
+    using S = value_store_t<VT>;
+    __shared__ float tops[T / kWave], sums_S[T / kWave], sums_T[T / kWave];
+    __shared__ Asked asked_room;
+    __shared__ std::conditional_t<DISTILL, Entries, int> entries;
+    __shared__ uint64_t keys[TOP ? T / kWave : 1][kWaiting];
+    const int64_t row = group_number();
+    if (row >= C.N) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
+    const S *x = (const S*)C.logits + row * C.V, *end = (const S*)C.logits + C.N * C.V;
+    const float c = C.scale * kLog2e;
+    RawUnit<VT> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int col = (threadIdx.x + u * T) * kRowUnit;
+        raw[u] = fetch_row_unit<VT>(x + col, C.V - col, end);
+    }
+    const Given given = row_given(C, row);
+    FewEntries<VT> few;
+    if constexpr (DISTILL) {
+        if (wave == 0 && C.k <= kFewEntries) few.ask(C, row, lane);
+    }
+    Asked asked = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (!DISTILL) asked = given_class<VT>(C, row, given);
+    float v[U][kRowUnit];
+#pragma unroll
+    for (int u = 0; u < U; ++u) unit_values<VT>(raw[u], C.V - (int)(threadIdx.x + u * T) * kRowUnit, -__builtin_inff(), v[u]);
+    Sums s = no_sums();
+    float lane_top = largest(v[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u) lane_top = fmaxf(lane_top, largest(v[u]));
+    if constexpr (DISTILL) {
+        if (wave == 0) {
+            asked = C.k <= kFewEntries ? few.take(C, lane, GRAD, entries) : take_more_entries<VT>(C, row, lane, entries);
+            if (lane == 0) asked_room = asked;
+        }
+    }
+    s.m = over_workgroup<T>(fmaxf(lane_top, kLowest), kMax, tops);
+    const auto distance = [&](float value) { return (value - s.m) * c; };
+    float e[U][kRowUnit];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) {
+            const float d = distance(v[u][j]);
+            e[u][j] = exp2_of(d);
+            s.S += e[u][j];
+            if constexpr (!DISTILL) s.T = fmaf(e[u][j], fmaxf(d, -kFar), s.T);
+        }
+    if constexpr (!DISTILL) s.T = over_lanes<kWave>(s.T, kAdd);
+    if (!DISTILL && lane == 0) sums_T[wave] = s.T;
+    s.S = over_workgroup<T>(s.S, kAdd, sums_S);
+    if constexpr (!DISTILL) s.T = over_lanes<T / kWave>(sums_T[threadIdx.x % (T / kWave)], kAdd);
+    if constexpr (DISTILL) asked = asked_room;
+    const Found f = row_results(C, given, s, asked);
+    if (threadIdx.x == 0) store_results(C, row, f);
+    if constexpr (TOP) {
+        Likeliest best;
+        best.begin(C.top_k, keys[wave], lane);
+        best.expect(lane_top, (int)threadIdx.x * kRowUnit < C.V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (threadIdx.x + u * T) * kRowUnit;
+            best.offer(v[u], largest(v[u]), col, C.V - col);
+        }
+        best.end();
+        const uint64_t key = merge_waves<T>(best.mine, keys, lane, wave);
+        if (wave == 0) store_likeliest(C, row, s, f.ln, fill<VT>(key, s, x, C.V, C.top_k, lane, keys[0]), lane);
+    }
+    if constexpr (GRAD) {
+        const Slope k = row_slope(C, given, s, asked, f);
+        S* dx = (S*)C.dlogits + row * C.V;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (threadIdx.x + u * T) * kRowUnit;
+            float g[kRowUnit];
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j) {
+                g[j] = e[u][j] * (DISTILL ? k.A : fmaf(k.B, fmaxf(distance(v[u][j]), -kFar), k.A));
+                if (!DISTILL && k.y == col + j) g[j] += k.g;
+            }
+            store_row_unit<VT>(dx + col, C.V - col, g);
+        }
+        if constexpr (DISTILL) {
+            __syncthreads();  // what is stored above at their columns is stored again
+            for (int i = threadIdx.x; i < C.k; i += T) {
+                const int col = entries.col[i];
+                if (col < 0) continue;
+                float q = entries.q[i];
+                bool mine = true;
+                if (C.k > kFewEntries) sum_of_column(C, entries, i, q, mine);
+                if (mine) dx[col] = round_value<VT>(fmaf(-k.g, q, exp2_of(distance(entries.x[i])) * k.A));
+            }
+        }
+    }
+}
+
 // ---- a workgroup a row ----
 
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
@@ -1383,6 +1495,14 @@ maxk_status run_teams(const ClassCall& C, hipStream_t s)
     return MAXK_OK;
 }
 
+template <int VT, int T, int U, bool DISTILL, bool GRAD, bool TOP>
+maxk_status run_held(const ClassCall& C, hipStream_t s)
+{
+    hipLaunchKernelGGL((class_held_kernel<VT, T, U, DISTILL, GRAD, TOP>), groups_of(C.N), dim3(T), 0, s, C);
+    MAXK_LAUNCH_CHECK();
+    return MAXK_OK;
+}
+
 template <int VT, int T, bool DISTILL, bool GRAD, bool TOP>
 maxk_status run_rows(const ClassCall& C, hipStream_t s)
 {
@@ -1437,9 +1557,19 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     if (units <= 64) return run_teams<VT, 64, 1, DISTILL, GRAD, TOP>(C, s);
     if (units <= 128) return run_teams<VT, 64, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
+    // Held and read once, or gone through twice?  us, held / gone through, gradient (alone): 40000 x 2500 bf16 104 (64) / 153 (99), fp32 149 (66) / 172 (100); 24396 x 4099 bf16 88 (54) /
+    // 124 (75); 12207 x 8192 bf16 75 (43) / 87 (44), fp32 143 / 178; 243 x 4099 4 / 6.  512 threads: 7142 x 14000 bf16 83 (42) / 95 (39), fp32 145 (68) / 190 (69), with alternatives
+    // 10 to 40 % more than without, but 365 x 8200 7 (5) / 12 (8), 16 / 29 with 50 of them.  1024 threads: 3571 x 28000 bf16 125 / 101.
+    if (units <= 512) return run_held<VT, 256, 2, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 768) return run_held<VT, 256, 3, DISTILL, GRAD, TOP>(C, s);
+    if (units <= 1024) return run_held<VT, 256, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
+    if (cut.segments == 1 && (GRAD || C.N <= 512)) {
+        if (units <= 1536) return run_held<VT, 512, 3, DISTILL, GRAD, TOP>(C, s);
+        if (units <= 2048) return run_held<VT, 512, 4, DISTILL, GRAD, TOP>(C, s);
+    }
     if (cut.segments == 1) {
-        const int T = C.N <= 512 && C.V >= 2 * kLeastSegment ? 1024 : C.N <= 1024 && C.V >= 2 * kLeastSegment ? 512 : GRAD ? threads_of<VT>(C.V) : kThreads;
+        const int T = C.N <= 512 ? 1024 : C.N <= 1024 ? 512 : GRAD ? threads_of<VT>(C.V) : kThreads;
         if (T == 1024) return run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s);
         if (T == 512) return run_rows<VT, 512, DISTILL, GRAD, TOP>(C, s);
         return run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);

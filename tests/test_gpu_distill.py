@@ -37,19 +37,19 @@ def check(x, data, index, dloss, temperature):
 
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
-@pytest.mark.parametrize("V", [1, 2, 7, 32, 47, 64, 65, 100, 256, 257, 512, 1000, 1025, 2048, 2500, 5003])
+@pytest.mark.parametrize("V", [1, 2, 7, 32, 47, 64, 65, 100, 256, 257, 512, 1000, 1025, 2048, 2500, 5003, 8191, 12001])
 def test_distill(V, dtype):
     for k, temperature, teacher in ((1, 1.0, torch.float32), (min(V, 16), 2.0, dtype), (min(V, 50), 0.5, torch.float16)):
         check(*inputs(33, V, k, dtype, V + k, teacher), temperature)
 
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
-@pytest.mark.parametrize("N,V,k", [(1, 32768, 20), (3, 131072, 64), (2, 50021, 1000), (600, 4099, 33), (1, 1, 1), (5, 9000, 1024), (1500, 300, 40), (3001, 47, 8)])
+@pytest.mark.parametrize("N,V,k", [(1, 32768, 20), (3, 131072, 64), (2, 50021, 1000), (600, 4099, 33), (600, 9001, 70), (150, 20003, 64), (1, 1, 1), (5, 9000, 1024), (1500, 300, 40), (3001, 47, 8)])
 def test_few_and_many_rows(N, V, k, dtype):
     check(*inputs(N, V, k, dtype, N + V + k), 4.0)
 
 
-@pytest.mark.parametrize("V", [40, 200, 1000, 3000, 9000])
+@pytest.mark.parametrize("V", [40, 200, 1000, 3000, 7000, 9000, 17000])
 def test_entries_that_are_none_or_several(V):
     """Columns outside the row, -Inf, rows without entries, columns that come more than once, logits that are masked out."""
     N, k = 12, 24

@@ -48,7 +48,7 @@ def check(x, labels, k=0, ib=torch.int32):
 
 
 # widths around a lane's, a team's, a wavefront's and a workgroup's columns and rounds
-WIDTHS = [1, 2, 5, 8, 9, 31, 32, 41, 47, 64, 65, 100, 128, 200, 256, 257, 500, 512, 513, 1000, 1024, 1025, 2000, 2048, 2049, 4095, 4097, 10007]
+WIDTHS = [1, 2, 5, 8, 9, 31, 32, 41, 47, 64, 65, 100, 128, 200, 256, 257, 500, 512, 513, 1000, 1024, 1025, 2000, 2048, 2049, 4095, 4097, 6145, 8193, 10007, 16383]
 
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
@@ -61,7 +61,7 @@ def test_logprobs(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
-@pytest.mark.parametrize("N,V", [(1, 32768), (3, 131072), (2, 50021), (700, 4099), (1, 1), (5, 9000), (64, 20011), (3001, 47), (1500, 300)])
+@pytest.mark.parametrize("N,V", [(1, 32768), (3, 131072), (2, 50021), (700, 4099), (1, 1), (5, 9000), (64, 20011), (3001, 47), (1500, 300), (600, 9001), (150, 16384), (520, 20003)])
 def test_few_and_many_rows(N, V, dtype):
     x, labels, _ = inputs(N, V, dtype, N + V)
     check(x, labels, min(V, 20))
@@ -212,7 +212,7 @@ def test_non_finite_rows_in_segments(V):
     assert torch.isnan(dx[[0, 1, 3]]).all()
 
 
-@pytest.mark.parametrize("V", [47, 300, 1500, 9000])
+@pytest.mark.parametrize("V", [47, 300, 1500, 3000, 9000])
 def test_non_finite(V):
     x = torch.zeros(4, V, device="cuda")
     x[0, V // 2] = NAN
@@ -229,7 +229,7 @@ def test_non_finite(V):
 
 
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
-@pytest.mark.parametrize("N,V", [(37, V) for V in WIDTHS] + [(1, 32768), (3, 70001), (700, 4099), (2, 131072), (3001, 47)])
+@pytest.mark.parametrize("N,V", [(37, V) for V in WIDTHS] + [(1, 32768), (3, 70001), (700, 4099), (2, 131072), (3001, 47), (600, 9001), (150, 16384), (520, 20003)])
 def test_gradient(N, V, dtype):
     x, labels, gen = inputs(N, V, dtype, 3 * V + N)
     g, u = (torch.randn(N, generator=gen, device="cuda") for _ in range(2))
@@ -252,7 +252,7 @@ def test_gradient(N, V, dtype):
 @pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
 def test_offsets(dtype):
     """Logits and gradients that start at any element; nothing is written around them."""
-    for N, V in ((9, 47), (5, 301), (7, 3001), (2, 9001)):
+    for N, V in ((9, 47), (5, 301), (7, 3001), (2, 9001), (130, 20001)):
         x, labels, gen = inputs(N, V, dtype, V, masked=False)
         g = torch.randn(N, generator=gen, device="cuda")
         want = torch.empty_like(x)
