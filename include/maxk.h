@@ -52,10 +52,10 @@ typedef int32_t maxk_status;
 enum {
     MAXK_OK = 0,
     MAXK_INVALID_ARGUMENT = -1, /* null pointer, negative size, k outside [1,dim], bad index_bytes, misaligned pointer */
-    MAXK_UNSUPPORTED = -2,      /* dim above MAXK_MAX_DIM, of the maxk_mx_* calls MAXK_MX_MAX_DIM */
+    MAXK_UNSUPPORTED = -2,      /* dim above MAXK_MAX_DIM, of the maxk_mx_* calls MAXK_MX_MAX_DIM; a width, N or k above what the call states (MAXK_NORM_MAX_DIM, MAXK_MAX_CLASSES, MAXK_MX_MATVEC_MAX_ROWS, MAXK_DISTILL_MAX_K) */
     MAXK_HIP_ERROR = -3,        /* a HIP call failed; see maxk_last_hip_error() */
     MAXK_OUT_OF_MEMORY = -4,
-    MAXK_SCRATCH_TOO_SMALL = -5 /* maxk_spgemm_fwd_noalloc: the graph's split rows need more than the fixed array; maxk_mx_weight_grad*: workspace_bytes is less than they need */
+    MAXK_SCRATCH_TOO_SMALL = -5 /* maxk_spgemm_fwd_noalloc: the graph's split rows need more than the fixed array; maxk_mx_weight_grad*, maxk_rms_norm_grad, maxk_logprobs*, maxk_distill*: workspace_bytes is less than they need */
 };
 
 /* Largest hidden width the kernels are compiled for. */

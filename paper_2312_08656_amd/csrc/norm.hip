@@ -4,7 +4,9 @@
 //   dx = r (dy gamma - x^ mean(dy gamma x^)) + dh,  x^ = h r;   dgamma = sum over rows of dy x^
 //
 // Streams: what they read and write once is what they cost.  L lanes have a row in their registers, U units of 8 columns each, so that it is read
-// once; for rows of up to 2048 columns that is part of a wavefront or all of it and no barrier is passed.
+// once; for rows of up to 2048 columns that is part of a wavefront or all of it and no barrier is passed.  716847 x 384 bf16 with residual and 8-bit codes 378 us, 5.1 TB/s;
+// 232965 x 256 fp32 182 and the gradient 202 (5.2 and 4.7; a copy: 5.0 to 5.1); 50000 x 4096 bf16 149 and 245.  Rows that are short and no whole 16-byte pieces leave lanes
+// idle and end in three stores: 2449029 x 47 bf16 148, where the memory would take 90.
 #include "heads.hpp"
 #include "rows.hpp"
 
@@ -15,7 +17,7 @@ constexpr int kThreads = 256;
 __host__ __device__ constexpr int norm_threads(int L) { return L > kThreads ? L : kThreads; }
 
 // Squares are added up in 64 bits: the sum does not depend on how a row is dealt to lanes beyond a rounding that is lost in r's, and codes that
-// lie next to a border between two come out the same on either side.  64-bit operations are a tenth of what the memory's time leaves room for.
+// lie next to a border between two come out the same on either side.  The vector units are busy for 47 % of 716847 x 384's time, for 17 % of fp32's.
 template <int VT, int L, int U>
 __global__ void __launch_bounds__(norm_threads(L)) norm_kernel(NormCall C, int64_t N, int dim)
 {
