@@ -1130,18 +1130,31 @@ struct Stretch {
         if (const int at = pieces * 16 + threadIdx.x; at < bytes) to[at] = room[place(at)];
     }
 };
-constexpr int kLaneRowLeast = 8;  // (four words a row and more: in_words)
-template <int VT, bool GRAD, bool ENTROPY>
+constexpr int kLaneRowLeast = 8;   // (four words a row and more: in_words)
+constexpr int kOwnEntries = 8;   // of a teacher, in the lane's registers
+template <int VT, bool DISTILL, bool GRAD, bool ENTROPY>
 __global__ void __launch_bounds__(kThreads) class_own_kernel(ClassCall C, Stretch R)
 {
     using S = value_store_t<VT>;
+    constexpr int K = DISTILL ? kOwnEntries : 1;
     extern __shared__ uint4 rooms_of_rows[];
     char* const rows = reinterpret_cast<char*>(rooms_of_rows);
     const int64_t row0 = group_number() * kThreads, row = row0 + threadIdx.x;
     if (row0 >= C.N) return;
     const int bytes = (int)min(C.N - row0, (int64_t)kThreads) * R.row;
     R.bring<sizeof(S) * kLaneRowMost / 16>((const char*)C.logits + row0 * R.row, bytes, rows);
-    const Given given = row_given(C, min(row, C.N - 1));
+    const int64_t known = min(row, C.N - 1);
+    const Given given = row_given(C, known);
+    int col[K];
+    float t[K], v[K];
+    if constexpr (DISTILL) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int64_t at = known * C.k + min(i, C.k - 1), there = column_of(C, at);
+            col[i] = i < C.k && there >= 0 && there < C.V ? (int)there : -1;
+            t[i] = teacher_value(C, at);
+        }
+    }
     __syncthreads();
     if (row < C.N) {
         S* const mine = reinterpret_cast<S*>(rows + threadIdx.x * R.pitch());
@@ -1155,7 +1168,32 @@ __global__ void __launch_bounds__(kThreads) class_own_kernel(ClassCall C, Stretc
             s.S += e;
             if constexpr (ENTROPY) s.T = fmaf(e, fmaxf(d, -kFar), s.T);
         }
-        const Asked asked = {given.y >= 0 && given.y < C.V ? widen_value<VT>(mine[given.y]) : 0.f, 0.f, 0.f, 0.f};
+        Asked asked = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (!DISTILL) asked.x = given.y >= 0 && given.y < C.V ? widen_value<VT>(mine[given.y]) : 0.f;
+        if constexpr (DISTILL) {
+            float top = kLowest, sum = 0.f;
+            asked.ref = kLowest;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                v[i] = col[i] >= 0 ? widen_value<VT>(mine[col[i]]) : -__builtin_inff();
+                t[i] = col[i] >= 0 ? t[i] : -__builtin_inff();
+                top = fmaxf(top, t[i]);
+                asked.ref = fmaxf(asked.ref, v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                t[i] = (t[i] - top) * c;
+                sum += exp2_of(t[i]);
+            }
+            const float ln = logf(sum), inverse = 1.f / sum;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const float q = sum == 0.f ? 0.f : exp2_of(t[i]) * inverse;
+                asked.C += q != 0.f ? q * (fmaf(kLn2, t[i], -ln) - (v[i] - asked.ref) * C.scale) : 0.f;
+                t[i] = q;
+            }
+            asked.Q = sum == 0.f ? 0.f : sum * inverse;
+        }
         const Found f = row_results(C, given, s, asked);
         store_results(C, row, f);
         if constexpr (GRAD) {
@@ -1164,7 +1202,31 @@ __global__ void __launch_bounds__(kThreads) class_own_kernel(ClassCall C, Stretc
 #pragma unroll 8
             for (int j = 0; j < C.V; ++j) {
                 const float d = (widen_value<VT>(mine[j]) - s.m) * c;
-                mine[j] = round_value<VT>(fmaf(exp2_of(d), ENTROPY ? fmaf(k.B, fmaxf(d, -kFar), k.A) : k.A, y == j ? k.g : 0.f));
+                mine[j] = round_value<VT>(fmaf(exp2_of(d), ENTROPY ? fmaf(k.B, fmaxf(d, -kFar), k.A) : k.A, !DISTILL && y == j ? k.g : 0.f));
+            }
+            if constexpr (DISTILL) {  // what is stored above at their columns is stored again
+                uint64_t columns = 0;
+                bool several = false;  // entries of one column
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    const uint64_t bit = col[i] >= 0 ? 1ull << col[i] : 0;
+                    several |= (columns & bit) != 0;
+                    columns |= bit;
+                }
+                float q[K];
+#pragma unroll
+                for (int i = 0; i < K; ++i) q[i] = t[i];
+                if (several) {
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        q[i] = 0.f;
+#pragma unroll
+                        for (int j = 0; j < K; ++j) q[i] += col[j] == col[i] ? t[j] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    if (col[i] >= 0) mine[col[i]] = round_value<VT>(fmaf(-k.g, q[i], exp2_of((v[i] - s.m) * c) * k.A));
             }
         }
     }
@@ -1522,16 +1584,17 @@ maxk_status run_lane_rows(const ClassCall& C, hipStream_t s)
     return MAXK_OK;
 }
 
-// Where rows leave a quarter and more of a team's columns idle and there are many of them.  us, a lane a row / a team, 2.45 M rows, log probabilities and gradient:
-// 9 bf16 32 / 60, 17 48 / 60, 33 87 / 118, 47 123 / 139 (alone, without a gradient, 59 / 83), 47 fp32 184 / 240; 32 bf16 87 / 64, 56 143 / 127, 64 162 / 130; 600 k rows: 9 11 / 18,
-// 33 27 / 32, 41 33 / 33; 170 k: 47 16 / 13
+// Where rows leave a quarter and more of a team's columns idle (distillation: an eighth) and there are many of them.  us, a lane a row / a team, 2.45 M rows, log
+// probabilities and gradient: 9 bf16 32 / 60, 17 48 / 60, 33 87 / 118, 47 123 / 139 (alone, without a gradient, 59 / 83), 47 fp32 184 / 240; 32 bf16 87 / 64, 56 143 / 127,
+// 64 162 / 130; 600 k rows: 9 11 / 18, 33 27 / 32, 41 33 / 33; 170 k: 47 16 / 13.  Distillation, 5 entries: 9 bf16 56 / 127, 33 130 / 207, 47 171 / 223, fp32 219 / 269, 24 137 /
+// 180, 48 217 / 248; 56 256 / 258, 64 290 / 265; 524 k rows: 33 34 / 48, 47 49 / 55.  (More entries, which a lane cannot hold, from LDS: 16 of 47 bf16 376 / 313.)
 constexpr int kManyOwnRows = 1 << 19;
-bool own_rows(int64_t N, int V) { return N >= kManyOwnRows && V >= kLaneRowLeast && 4 * V < 3 * (V <= 4 * kRowUnit ? 4 : 8) * kRowUnit; }
-template <int VT, bool GRAD, bool ENTROPY>
+bool own_rows(int64_t N, int V, int eighths) { return N >= kManyOwnRows && V >= kLaneRowLeast && 8 * V < eighths * (V <= 4 * kRowUnit ? 4 : 8) * kRowUnit; }
+template <int VT, bool DISTILL, bool GRAD, bool ENTROPY>
 maxk_status run_own_rows(const ClassCall& C, hipStream_t s)
 {
     const Stretch R = Stretch::of(C.V, sizeof(value_store_t<VT>));
-    hipLaunchKernelGGL((class_own_kernel<VT, GRAD, ENTROPY>), groups_of((C.N + kThreads - 1) / kThreads), dim3(kThreads), R.room(), s, C, R);
+    hipLaunchKernelGGL((class_own_kernel<VT, DISTILL, GRAD, ENTROPY>), groups_of((C.N + kThreads - 1) / kThreads), dim3(kThreads), R.room(), s, C, R);
     MAXK_LAUNCH_CHECK();
     return MAXK_OK;
 }
@@ -1546,9 +1609,12 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
             if (keys <= 6) return run_lane_rows<VT, 6>(C, s);
             return run_lane_rows<VT, kLaneRowKeys>(C, s);
         }
-    if constexpr (!TOP && !DISTILL)
-        if (own_rows(C.N, C.V))
-            return C.entropy || C.dentropy ? run_own_rows<VT, GRAD, true>(C, s) : run_own_rows<VT, GRAD, false>(C, s);
+    if constexpr (!TOP)
+        if (own_rows(C.N, C.V, DISTILL ? 7 : 6) && (!DISTILL || C.k <= kOwnEntries)) {
+            if constexpr (!DISTILL)
+                if (C.entropy || C.dentropy) return run_own_rows<VT, DISTILL, GRAD, true>(C, s);
+            return run_own_rows<VT, DISTILL, GRAD, false>(C, s);
+        }
     const int units = (C.V + kRowUnit - 1) / kRowUnit;
     if (units <= 4) return run_teams<VT, 4, 1, DISTILL, GRAD, TOP>(C, s);
     if (units <= 8) return run_teams<VT, 8, 1, DISTILL, GRAD, TOP>(C, s);

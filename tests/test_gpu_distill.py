@@ -76,6 +76,43 @@ def test_entries_that_are_none_or_several(V):
     assert loss[8] == INF and loss[9] == 0 and (grad[8:10] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("V,k", [(8, 8), (9, 1), (16, 5), (23, 8), (24, 3), (27, 9), (33, 2), (40, 8), (47, 5), (47, 8), (55, 7)])
+def test_many_short_rows(V, k, dtype):
+    """Rows enough for the form with a lane a row (nine entries: not); a last workgroup that is not full, entries that are none or several, any element's alignment."""
+    N = (1 << 19) + 225
+    for index_type, teacher in ((torch.uint8, dtype), (torch.int32, torch.float32), (torch.uint16, torch.float16)):
+        x, data, index, dloss = inputs(N, V, k, dtype, V + k, teacher)
+        index = index.to(torch.int32)
+        index[:20] = torch.randint(V, (20, k), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).int()
+        index[20, 0] = V
+        data[21, k // 2] = -INF
+        data[22] = -INF
+        index[23] = 255
+        x[24, index[24, k - 1].item()] = -INF
+        x[25] = -INF
+        x[26] = -INF
+        index[26] = 255
+        x[27] = torch.finfo(dtype).min
+        index = index.to(index_type)
+        some = torch.cat([torch.arange(150), torch.arange(N - 300, N)]).cuda()
+        want, bound, dx, dx_bound = hc.distill(x[some], data[some], index.to(torch.int32)[some], 2.0, dloss[some])
+        loss, only, grad = torch.full((N,), 7.0, device="cuda"), torch.full((N,), 7.0, device="cuda"), torch.full_like(x, 7)
+        maxk.maxk_distill(x, data, index, only, 2.0)
+        maxk.maxk_distill_grad(x, data, index, dloss, grad, 2.0, loss)
+        assert torch.equal(loss, only)
+        hc.close(loss[some], want, bound)
+        hc.close(grad[some], dx, dx_bound, dtype)
+        assert (loss[22:24] == 0).all() and loss[24] == INF and loss[25] == INF and loss[26] == 0 and (grad[[22, 23, 25, 26]] == 0).all()
+        flat, out = (torch.full((N * V + 16,), 3.0, dtype=dtype, device="cuda") for _ in range(2))
+        flat[3:3 + N * V].copy_(x.view(-1))
+        moved = out[1:1 + N * V].view(N, V)
+        maxk.maxk_distill_grad(flat[3:3 + N * V].view(N, V), data, index, dloss, moved, 2.0)
+        assert torch.equal(moved, grad) and out[0] == 3 and (out[1 + N * V:] == 3).all()
+        maxk.maxk_distill_grad(x, data, index, dloss, x, 2.0)  # in the logits' own memory
+        assert torch.equal(x, grad)
+
+
 def test_non_finite():
     x, data, index, dloss = inputs(5, 60, 6, torch.float32, 3)
     x[0, 10] = float("nan")

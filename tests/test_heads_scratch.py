@@ -6,7 +6,7 @@ import pytest
 from paper_2312_08656_amd import binding
 from test_scratch import code_objects
 
-LEAST = {"norm_kernel": 39, "norm_grad_kernel": 39, "add_parts_kernel": 1, "class_team_kernel": 100, "class_lane_kernel": 12, "class_own_kernel": 12, "class_held_kernel": 75, "class_rows_kernel": 45, "class_parts_kernel": 9,
+LEAST = {"norm_kernel": 39, "norm_grad_kernel": 39, "add_parts_kernel": 1, "class_team_kernel": 100, "class_lane_kernel": 12, "class_own_kernel": 18, "class_held_kernel": 75, "class_rows_kernel": 45, "class_parts_kernel": 9,
          "class_join_kernel": 6, "class_gradient_kernel": 6, "matvec_kernel": 6, "matvec_lanes_kernel": 40}
 
 KNOWN = "norm_grad_kernelILi0ELi1024ELi2E"  # fp32 rows of 8193 to 16384 columns: 2 registers
