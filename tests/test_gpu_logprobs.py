@@ -304,6 +304,28 @@ def test_rows_past_32_bits():
     assert ((x[:, -1].float() + 1 / S).abs() <= 2.0 ** -8 / S + 1e-9).all()
 
 
+@pytest.mark.parametrize("N", [2, 130])
+def test_most_classes(N):
+    V = 1 << 24
+    x = torch.zeros(N, V, dtype=torch.float16, device="cuda")
+    places = torch.tensor([V - 1, 77, V // 2, 5_000_011], device="cuda")
+    x[:, places] = torch.tensor([12.0, 11.0, 10.0, 9.0], dtype=torch.float16, device="cuda")
+    labels = torch.full((N,), V - 1, device="cuda")
+    labels[1] = V + (1 << 33)
+    logprob, entropy, data, index = results(N, 6)
+    maxk.maxk_logprobs(x, labels, logprob, entropy, data, index)
+    e = np.exp([12.0, 11.0, 10.0, 9.0])
+    S = e.sum() + V - 4
+    H = np.log(S) - (e * [12.0, 11.0, 10.0, 9.0]).sum() / S
+    # 2^24 ones are added up exactly in any order; the other roundings are those of a few terms and of two logarithms of less than 17
+    assert abs(logprob[0].item() - (12 - np.log(S))) < 64 * 17 * hc.U and torch.isnan(logprob[1]) and abs(entropy[0].item() - H) < 64 * 17 * hc.U
+    assert (index == torch.tensor([V - 1, 77, V // 2, 5_000_011, 0, 1], device="cuda")).all()
+    maxk.maxk_logprobs_grad(x, x, labels.clamp_max(V - 1), torch.ones(N, device="cuda"))
+    p = e[1] / S
+    assert abs(x[N - 1, 77].item() + p) <= 2.0 ** -11 * p + 1e-6 and abs(x[0, V - 1].item() - (1 - e[0] / S)) <= 2.0 ** -11 + 1e-6
+    assert abs(x[N - 1, V // 4].item() + 1 / S) <= 2.0 ** -25 + 1e-12
+
+
 def test_as_many_rows_as_fit_no_launch_of_one_dimension():
     """Four lanes a row: 2^30 rows are 2^32 threads."""
     N = (1 << 30) + 12_345

@@ -59,6 +59,29 @@ def test_many_columns_and_rows(din, dout):
         check(torch.from_numpy(mx_common.features(rng, N, din)).cuda().to(dtype), codes, scales, W, None, dtype)
 
 
+def test_most_rows():
+    rng = np.random.default_rng(9)
+    codes, scales, W = weights(rng, 300, 1030)
+    for N, dtype in ((1024, torch.float32), (1000, torch.bfloat16), (129, torch.float16)):
+        check(torch.from_numpy(mx_common.features(rng, N, 1030)).cuda().to(dtype), codes, scales, W, None, dtype)
+
+
+def test_more_workgroups_than_a_launch_of_one_dimension_has():
+    """A row of X by four rows of W a workgroup of 1024 threads: 2^22 rows are 2^30 threads, past them the grid's second dimension begins; codes and offsets past 2^32 bytes."""
+    din, dout = 16416, (1 << 22) + 5
+    codes, scales = torch.zeros(dout, din // 2, dtype=torch.uint8, device="cuda"), torch.full((dout, din // 32), 127, dtype=torch.uint8, device="cuda")
+    some = [0, 3, (1 << 20) + 1, (1 << 22) - 1, 1 << 22, dout - 1]
+    for i, o in enumerate(some):
+        codes[o, 1000 + i] = 0x2A  # the even column -1, the odd one 1
+        codes[o, din // 2 - 1] = 0x60  # the last column 4
+    X = torch.arange(din, device="cuda", dtype=torch.float32).view(1, din)
+    Y = torch.full((1, dout), 7.0, device="cuda")
+    maxk.maxk_mx_matvec(X, codes, scales, Y)
+    assert torch.equal(Y[0, some], torch.full((len(some),), 1.0 + 4 * (din - 1), device="cuda"))
+    Y[0, some] = 0
+    assert not Y.any()
+
+
 def test_offsets_and_what_lies_around():
     rng = np.random.default_rng(4)
     N, din, dout = 3, 77, 45
