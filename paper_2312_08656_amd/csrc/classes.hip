@@ -842,39 +842,105 @@ __device__ __forceinline__ void likeliest_in_turn(const ClassCall& C, int64_t ro
     }
 }
 
-// A column's place is the number of columns with a greater value, or an equal one to the left of it: of those to the left a value counts that is greater than this one's
-// key less 1.  (room: the row's keys in LDS.  Keys from 1 on: 0 is behind the row's end)
-template <int L>
-__device__ __forceinline__ void likeliest_by_place(const ClassCall& C, int64_t row, const Sums& s, float ln, const float (&v)[kRowUnit], int lane, uint32_t* room)
+// Keys of a row in order: of fp32 as above, of 16-bit values, which leave the last 12 bits of theirs alone, in 32 bits with the column (rows are of up to 256) in the last 8.
+template <int VT>
+__device__ __forceinline__ auto short_key(float x, int col)
 {
-    uint32_t key[kRowUnit];
-    int place[kRowUnit];
-#pragma unroll
-    for (int j = 0; j < kRowUnit; ++j) {
-        key[j] = lane * kRowUnit + j < C.V ? max(value_key(v[j]), 1u) : 0u;
-        place[j] = 0;
-    }
-    *reinterpret_cast<uint4*>(room + lane * kRowUnit) = make_uint4(key[0], key[1], key[2], key[3]);
-    *reinterpret_cast<uint4*>(room + lane * kRowUnit + 4) = make_uint4(key[4], key[5], key[6], key[7]);
-    wave_fence();
-    for (int part = 0; part * kRowUnit < C.V; ++part) {
-        const uint4 a = *reinterpret_cast<const uint4*>(room + part * kRowUnit), b = *reinterpret_cast<const uint4*>(room + part * kRowUnit + 4);
-        const uint32_t other[kRowUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int j = 0; j < kRowUnit; ++j) {
-            const uint32_t over = part < lane ? key[j] - 1u : part > lane ? key[j] : 0xFFFFFFFFu;  // (its own columns: below)
-#pragma unroll
-            for (int i = 0; i < kRowUnit; ++i) place[j] += other[i] > over;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kRowUnit; ++j)
-#pragma unroll
-        for (int i = 0; i < kRowUnit; ++i) place[j] += i < j ? key[i] >= key[j] : key[i] > key[j];
-#pragma unroll
-    for (int j = 0; j < kRowUnit; ++j)
-        if (lane * kRowUnit + j < C.V && place[j] < C.top_k) store_likeliest(C, row, s, ln, key_of(v[j], (uint32_t)(lane * kRowUnit + j)), place[j]);
+    if constexpr (VT == MAXK_VALUE_F32) return pair_key(x, col);
+    else return (value_key(x) & ~0xFFu) | (uint32_t)(255 - col);
 }
+__device__ __forceinline__ uint64_t long_key(double key) { return unpaired(key); }
+__device__ __forceinline__ uint64_t long_key(uint32_t key)  // (the value's last bits: as those of a negative one, or none)
+{
+    const uint32_t v = key & ~0xFFu;
+    return (uint64_t)(v & 0x80000000u ? v : v | 0xFFu) << 32 | (0xFFFFFFFFu - (255 - (key & 0xFFu)));
+}
+__device__ __forceinline__ uint32_t greater_of(uint32_t a, uint32_t b) { return max(a, b); }
+__device__ __forceinline__ uint32_t lesser_of(uint32_t a, uint32_t b) { return min(a, b); }
+template <typename K>
+__device__ __forceinline__ void in_order(K& a, K& b)
+{
+    const K less = lesser_of(a, b);
+    a = greater_of(a, b);
+    b = less;
+}
+// of lane ^ X, X all ones (a group's lanes from its other end) or one bit
+template <int X>
+__device__ __forceinline__ uint32_t partner(uint32_t x)
+{
+    if constexpr (X == 3) return dpp<0x1B>(x);                // quad_perm [3,2,1,0]
+    else if constexpr (X == 7) return dpp<0x141>(x);          // row_half_mirror
+    else if constexpr (X == 15) return dpp<0x140>(x);         // row_mirror
+    else if constexpr (X == 31) return across<16>(dpp<0x140>(x));
+    else return across<X>(x);
+}
+template <int X>
+__device__ __forceinline__ double partner(double x)
+{
+    return __hiloint2double((int)partner<X>((uint32_t)__double2hiint(x)), (int)partner<X>((uint32_t)__double2loint(x)));
+}
+template <typename K>
+__device__ __forceinline__ K end_of(K mine, K other, bool greater) { return greater ? greater_of(mine, other) : lesser_of(mine, other); }
+// runs of eight in a lane whose halves are neither before nor behind each other in order, once their greater and lesser ones are apart
+template <int STEP, typename K>
+__device__ __forceinline__ void settle_unit(K (&key)[kRowUnit])
+{
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j)
+        if ((j & STEP) == 0) in_order(key[j], key[j + STEP]);
+    if constexpr (STEP > 1) settle_unit<STEP / 2>(key);
+}
+template <int STEP, typename K>
+__device__ __forceinline__ void settle_lanes(K (&key)[kRowUnit], int lane)
+{
+    if constexpr (STEP > 0) {
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) key[j] = end_of(key[j], partner<STEP>(key[j]), (lane & STEP) == 0);
+        settle_lanes<STEP / 2>(key, lane);
+    }
+}
+// Two groups of M lanes, each in order, into one: the first against the last of the other, the second against the last but one ...
+template <int M, int L, typename K>
+__device__ __forceinline__ void merge_groups(K (&key)[kRowUnit], int lane)
+{
+    if constexpr (M < L) {
+        K other[kRowUnit];
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) other[j] = partner<2 * M - 1>(key[kRowUnit - 1 - j]);
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j) key[j] = end_of(key[j], other[j], (lane & M) == 0);
+        settle_lanes<M / 2>(key, lane);
+        settle_unit<4>(key);
+        merge_groups<2 * M, L>(key, lane);
+    }
+}
+template <int VT, int L>
+__device__ __forceinline__ void likeliest_in_order(const ClassCall& C, int64_t row, const Sums& s, float ln, const float (&v)[kRowUnit], int lane)
+{
+    using K = decltype(short_key<VT>(0.f, 0));
+    K key[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) key[j] = lane * kRowUnit + j < C.V ? short_key<VT>(v[j], lane * kRowUnit + j) : K(0);
+#pragma unroll
+    for (int size = 2; size <= kRowUnit; size *= 2) {
+#pragma unroll
+        for (int j = 0; j < kRowUnit; ++j)
+            if ((j & (size / 2)) == 0) in_order(key[j], key[j ^ (size - 1)]);
+#pragma unroll
+        for (int step = size / 4; step > 0; step /= 2)
+#pragma unroll
+            for (int j = 0; j < kRowUnit; ++j)
+                if ((j & step) == 0) in_order(key[j], key[j + step]);
+    }
+    merge_groups<1, L>(key, lane);
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) store_likeliest(C, row, s, ln, long_key(key[j]), lane * kRowUnit + j);
+}
+
+// Rounds cost some sixty instructions for each alternative, an order of the whole row 150 to 400.  us, in turn / in order: 150000 x 200 bf16 1 alternative 41 / 98, 12 105 / 118,
+// 16 130 / 117, 64 426 / 118; 300000 x 100 fp32 12 93 / 97, 16 112 / 98, 64 279 / 100; 500000 x 47 bf16 10 69 / 66, fp32 12 79 / 71; 1500000 x 20 8 17 / 13 (130000 rows).
+template <int L> constexpr int kFewInTurn = L == 4 ? 7 : L == 8 ? 10 : 13;
+
 
 struct Nothing {
     __device__ __forceinline__ Nothing(const ClassCall&, int64_t, int, float*) {}
@@ -887,7 +953,6 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
     constexpr int kTeams = kThreads / L;
     __shared__ __attribute__((aligned(16))) float spread[DISTILL && GRAD ? kTeams * L * U * kRowUnit : 1];
     __shared__ uint64_t keys[TOP && L == kWave ? kThreads / kWave : 1][TOP && L == kWave ? kWaiting : 1];
-    __shared__ __attribute__((aligned(16))) uint32_t places[TOP && L < kWave ? kThreads * kRowUnit : 1];
     const int lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t row = group_number() * kTeams + team;
     if (row >= C.N) return;
@@ -948,9 +1013,8 @@ __global__ void __launch_bounds__(kThreads) class_team_kernel(ClassCall C)
         store_likeliest(C, row, s, f.ln, fill<VT>(best.mine, s, x, C.V, C.top_k, lane, keys[team]), lane);
     } else if constexpr (TOP) {
         static_assert(U == 1);
-        // Few alternatives in rounds, some fifty instructions each; many by their places, 18 instructions a column.  us, 27685 rows of 41 bf16 with all of them, 21 / 12
-        if (3 * C.top_k < C.V) likeliest_in_turn<L>(C, row, s, f.ln, v[0], lane);
-        else likeliest_by_place<L>(C, row, s, f.ln, v[0], lane, places + team * L * kRowUnit);
+        if (C.top_k < kFewInTurn<L>) likeliest_in_turn<L>(C, row, s, f.ln, v[0], lane);
+        else likeliest_in_order<VT, L>(C, row, s, f.ln, v[0], lane);
     }
     if constexpr (GRAD) {
         const Slope k = row_slope(C, given, s, asked, f);

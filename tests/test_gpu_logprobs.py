@@ -75,6 +75,21 @@ def test_alternatives(k, V):
         check(x, labels, k, torch.uint8 if V <= 256 else torch.uint16 if k % 2 else torch.int32)
 
 
+@pytest.mark.parametrize("dtype", hc.TYPES, ids=str)
+@pytest.mark.parametrize("V", [2, 7, 8, 13, 31, 32, 33, 47, 64, 65, 127, 128, 129, 200, 255, 256])
+def test_alternatives_of_short_rows(V, dtype):
+    """Every number of them up to the row's end or 64, over more than one wavefront; masked ones and equal ones among them."""
+    x, labels, gen = inputs(70, V, dtype, V)
+    x[10:40] = torch.randint(-3, 4, (30, V), generator=gen, device="cuda").to(dtype)
+    x[20:30, ::2] = -INF
+    x[40] = torch.where(torch.arange(V, device="cuda") % 3 == 0, -0.0, 0.0).to(dtype)
+    x[41] = torch.finfo(dtype).min
+    x[42] = torch.finfo(dtype).smallest_normal * torch.randint(-9, 9, (V,), generator=gen, device="cuda").to(dtype) / 16
+    for k in {1, 2, 6, 7, 9, 10, 12, 13, 20, 40, 64, V}:
+        if k <= min(V, 64):
+            check(x, labels, k, torch.uint8)
+
+
 @pytest.mark.parametrize("V", [40, 130, 600, 1500, 3000, 30000])
 def test_alternatives_in_any_order(V):
     """Rows that rise, fall, are all the same, have the largest last or hold few different values."""
