@@ -428,16 +428,22 @@ __device__ __forceinline__ void store_results(const ClassCall& C, int64_t row, c
     if (C.loss) C.loss[row] = f.loss;
 }
 
+struct Alternative { float logprob; uint32_t col; };
+__device__ __forceinline__ Alternative alternative(const Sums& s, float ln, uint64_t key, int i)
+{
+    const float x = key_value((uint32_t)(key >> 32));
+    return {key == 0 || s.S != s.S ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (x - s.m) - ln,
+            key ? 0xFFFFFFFFu - (uint32_t)key : (uint32_t)i};  // (a row of NaN leaves none)
+}
 __device__ __forceinline__ void store_likeliest(const ClassCall& C, int64_t row, const Sums& s, float ln, uint64_t key, int i)
 {
     if (i >= C.top_k) return;
     const int64_t at = row * C.top_k + i;
-    const uint32_t col = key ? 0xFFFFFFFFu - (uint32_t)key : (uint32_t)i;  // (a row of NaN leaves none)
-    const float x = key_value((uint32_t)(key >> 32));
-    C.top_data[at] = key == 0 || s.S != s.S ? __builtin_nanf("") : s.S == 0.f ? -__builtin_inff() : (x - s.m) - ln;
-    if (C.top_index_bytes == 1) ((uint8_t*)C.top_index)[at] = (uint8_t)col;
-    else if (C.top_index_bytes == 2) ((uint16_t*)C.top_index)[at] = (uint16_t)col;
-    else ((uint32_t*)C.top_index)[at] = col;
+    const Alternative a = alternative(s, ln, key, i);
+    C.top_data[at] = a.logprob;
+    if (C.top_index_bytes == 1) ((uint8_t*)C.top_index)[at] = (uint8_t)a.col;
+    else if (C.top_index_bytes == 2) ((uint16_t*)C.top_index)[at] = (uint16_t)a.col;
+    else ((uint32_t*)C.top_index)[at] = a.col;
 }
 
 // dx = e (A + B d) + g at the given class
@@ -933,12 +939,25 @@ __device__ __forceinline__ void likeliest_in_order(const ClassCall& C, int64_t r
                 if ((j & step) == 0) in_order(key[j], key[j + step]);
     }
     merge_groups<1, L>(key, lane);
+    float data[kRowUnit];
+    uint32_t index[kRowUnit];
+    uint16_t short_index[kRowUnit];
+    uint8_t byte_index[kRowUnit];
 #pragma unroll
-    for (int j = 0; j < kRowUnit; ++j) store_likeliest(C, row, s, ln, long_key(key[j]), lane * kRowUnit + j);
+    for (int j = 0; j < kRowUnit; ++j) {
+        const Alternative a = alternative(s, ln, long_key(key[j]), lane * kRowUnit + j);
+        data[j] = a.logprob, index[j] = a.col, short_index[j] = (uint16_t)a.col, byte_index[j] = (uint8_t)a.col;
+    }
+    const int64_t at = row * C.top_k + lane * kRowUnit;
+    const int valid = C.top_k - lane * kRowUnit;
+    store_values(C.top_data + at, valid, data);
+    if (C.top_index_bytes == 1) store_values((uint8_t*)C.top_index + at, valid, byte_index);
+    else if (C.top_index_bytes == 2) store_values((uint16_t*)C.top_index + at, valid, short_index);
+    else store_values((uint32_t*)C.top_index + at, valid, index);
 }
 
-// Rounds cost some sixty instructions for each alternative, an order of the whole row 150 to 400.  us, in turn / in order: 150000 x 200 bf16 1 alternative 41 / 98, 12 105 / 118,
-// 16 130 / 117, 64 426 / 118; 300000 x 100 fp32 12 93 / 97, 16 112 / 98, 64 279 / 100; 500000 x 47 bf16 10 69 / 66, fp32 12 79 / 71; 1500000 x 20 8 17 / 13 (130000 rows).
+// Rounds cost some sixty instructions for each alternative, an order of the whole row 150 to 400.  us, in turn / in order: 150000 x 200 bf16 1 alternative 41 / 98, 12 105 / 107,
+// 16 130 / 107, 64 426 / 108; 300000 x 100 fp32 12 93 / 94, 16 112 / 94, 64 279 / 95; 500000 x 47 bf16 10 69 / 59, fp32 12 79 / 70; 130000 x 20 bf16 8 16 / 10.
 template <int L> constexpr int kFewInTurn = L == 4 ? 7 : L == 8 ? 10 : 13;
 
 

@@ -105,12 +105,10 @@ __device__ __forceinline__ void load_row_unit(const value_store_t<VT>* p, int va
     unit_values<VT>(fetch_row_unit<VT>(p, valid, end), valid, fill, x);
 }
 
-template <int VT>
-__device__ __forceinline__ void store_row_unit(value_store_t<VT>* p, int valid, const float (&x)[kRowUnit])
+// A lane's unit at p, of which `valid` elements (less than 1: none) belong to the row
+template <typename T>
+__device__ __forceinline__ void store_values(T* p, int valid, const T (&v)[kRowUnit])
 {
-    value_store_t<VT> v[kRowUnit];
-#pragma unroll
-    for (int j = 0; j < kRowUnit; ++j) v[j] = round_value<VT>(x[j]);
     if (valid >= kRowUnit) {
         __builtin_memcpy(p, v, sizeof(v));
         return;
@@ -118,13 +116,22 @@ __device__ __forceinline__ void store_row_unit(value_store_t<VT>* p, int valid, 
     // a row's last columns: four, two and one of them
     const bool four = valid >= 4, two = valid > 0 && (valid & 2), one = valid > 0 && (valid & 1);
     if (four) __builtin_memcpy(p, v, 4 * sizeof(v[0]));
-    const value_store_t<VT> a = four ? v[4] : v[0], b = four ? v[5] : v[1], c = four ? v[6] : v[2];
+    const T v0 = v[0], v1 = v[1], v2 = v[2], v4 = v[4], v5 = v[5], v6 = v[6];  // (values: of two places in an array one would be taken in memory)
+    const T a = four ? v4 : v0, b = four ? v5 : v1, c = four ? v6 : v2;
     const int at = four ? 4 : 0;
     if (two) {
-        const value_store_t<VT> pair[2] = {a, b};
+        const T pair[2] = {a, b};
         __builtin_memcpy(p + at, pair, sizeof(pair));
     }
     if (one) p[two ? at + 2 : at] = two ? c : a;
+}
+template <int VT>
+__device__ __forceinline__ void store_row_unit(value_store_t<VT>* p, int valid, const float (&x)[kRowUnit])
+{
+    value_store_t<VT> v[kRowUnit];
+#pragma unroll
+    for (int j = 0; j < kRowUnit; ++j) v[j] = round_value<VT>(x[j]);
+    store_values(p, valid, v);
 }
 
 // ---- over the L lanes (a power of two, up to 64) that share a row: every lane has the result, the same bits ----
