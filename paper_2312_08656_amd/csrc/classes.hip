@@ -224,14 +224,24 @@ struct Likeliest {
     }
     // The k-th greatest of the lanes' largest values is no less than the k-th greatest value of all: a first bound, its leading 20 bits, before anything is
     // offered.  (any: the lane has one)
-    __device__ __forceinline__ void expect(float top, bool any)
+    static __device__ __forceinline__ uint32_t head(float top, bool any) { return any && top > -__builtin_inff() ? value_key(top) : 0u; }
+    template <int R>
+    __device__ __forceinline__ void expect(const uint32_t (&heads)[R])  // of R wavefronts
     {
-        const uint32_t key = any && top > -__builtin_inff() ? value_key(top) : 0u;
         uint32_t bound = 0;
 #pragma unroll
-        for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1)
-            if (__popcll(__ballot(key >= (bound | bit))) >= k) bound |= bit;
+        for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1) {
+            int n = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) n += __popcll(__ballot(heads[r] >= (bound | bit)));
+            if (n >= k) bound |= bit;
+        }
         raise((uint64_t)bound << 32);
+    }
+    __device__ __forceinline__ void expect(float top, bool any)
+    {
+        const uint32_t heads[1] = {head(top, any)};
+        expect(heads);
     }
     // a unit at column `col`: all lanes come here, those without columns with valid < 1
     __device__ __forceinline__ void offer(const float (&x)[kRowUnit], float top, int col, int valid)
@@ -1340,6 +1350,7 @@ __global__ void __launch_bounds__(T) class_held_kernel(ClassCall C)
     __shared__ Asked asked_room;
     __shared__ std::conditional_t<DISTILL, Entries, int> entries;
     __shared__ uint64_t keys[TOP ? T / kWave : 1][kWaiting];
+    __shared__ uint32_t heads[TOP ? T : 1];
     const int64_t row = group_number();
     if (row >= C.N) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave;
@@ -1371,6 +1382,7 @@ __global__ void __launch_bounds__(T) class_held_kernel(ClassCall C)
             if (lane == 0) asked_room = asked;
         }
     }
+    if constexpr (TOP) heads[threadIdx.x] = Likeliest::head(lane_top, (int)threadIdx.x * kRowUnit < C.V);
     s.m = over_workgroup<T>(fmaxf(lane_top, kLowest), kMax, tops);
     const auto distance = [&](float value) { return (value - s.m) * c; };
     float e[U][kRowUnit];
@@ -1393,7 +1405,11 @@ __global__ void __launch_bounds__(T) class_held_kernel(ClassCall C)
     if constexpr (TOP) {
         Likeliest best;
         best.begin(C.top_k, keys[wave], lane);
-        best.expect(lane_top, (int)threadIdx.x * kRowUnit < C.V);
+        uint32_t all[T / kWave];  // (the whole row's lanes: of 2500 columns' 50 greatest keys a wavefront then has 15 instead of 70.  16000 rows
+        // of them, bf16: 76 us, 123 with a bound of its own)
+#pragma unroll
+        for (int r = 0; r < T / kWave; ++r) all[r] = heads[lane + r * kWave];
+        best.expect(all);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (threadIdx.x + u * T) * kRowUnit;
@@ -1707,13 +1723,13 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     if (units <= 128) return run_teams<VT, 64, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
     // Held and read once, or gone through twice?  us, held / gone through, gradient (alone): 40000 x 2500 bf16 104 (64) / 153 (99), fp32 149 (66) / 172 (100); 24396 x 4099 bf16 88 (54) /
-    // 124 (75); 12207 x 8192 bf16 75 (43) / 87 (44), fp32 143 / 178; 243 x 4099 4 / 6.  512 threads: 7142 x 14000 bf16 83 (42) / 95 (39), fp32 145 (68) / 190 (69), with alternatives
-    // 10 to 40 % more than without, but 365 x 8200 7 (5) / 12 (8), 16 / 29 with 50 of them.  1024 threads: 3571 x 28000 bf16 125 / 101.
+    // 124 (75); 12207 x 8192 bf16 75 (43) / 87 (44), fp32 143 / 178; 243 x 4099 4 / 6.  512 threads: 7142 x 14000 bf16 83 (42) / 95 (39), fp32 145 (68) / 190 (69);
+    // 4444 x 9000 bf16 with 5 alternatives 57 / 35, 20 61 / 55, 50 65 / 77, fp32 70 / 96, 2500 x 16000 bf16 44 / 60; 365 x 8200 gradient 7 (5) / 12 (8).  1024 threads: 3571 x 28000 bf16 125 / 101.
     if (units <= 512) return run_held<VT, 256, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 768) return run_held<VT, 256, 3, DISTILL, GRAD, TOP>(C, s);
     if (units <= 1024) return run_held<VT, 256, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
-    if (cut.segments == 1 && (GRAD || C.N <= 512)) {
+    if (cut.segments == 1 && (GRAD || C.N <= 512 || C.top_k >= 24)) {
         if (units <= 1536) return run_held<VT, 512, 3, DISTILL, GRAD, TOP>(C, s);
         if (units <= 2048) return run_held<VT, 512, 4, DISTILL, GRAD, TOP>(C, s);
     }

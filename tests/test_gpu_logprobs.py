@@ -65,10 +65,11 @@ def test_logprobs(V, dtype):
 def test_few_and_many_rows(N, V, dtype):
     x, labels, _ = inputs(N, V, dtype, N + V)
     check(x, labels, min(V, 20))
+    check(x, labels, min(V, 30))
 
 
 @pytest.mark.parametrize("k", [1, 2, 3, 7, 16, 33, 50, 63, 64])
-@pytest.mark.parametrize("V", [64, 65, 100, 256, 700, 1500, 5000, 40000])
+@pytest.mark.parametrize("V", [64, 65, 100, 256, 700, 1500, 5000, 9001, 16000, 40000])
 def test_alternatives(k, V):
     for dtype in (torch.float32, torch.bfloat16):  # (many equal values in 16 bits)
         x, labels, _ = inputs(9, V, dtype, k + V)
