@@ -6,7 +6,10 @@
 //
 // Rows of up to 2048 columns lie in the registers of a part of a wavefront or of all of it, of up to 16384 in a workgroup's, and are read once.  One pass over a longer row
 // has its maximum and sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end; the gradient reads the row again, from the caches, and
-// writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.
+// writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.  Many short rows go through LDS, where a lane has one of them.
+//
+// Bound by memory from 64 columns on (169343 x 1000 fp32, distillation 251 us, 5.5 TB/s; 4096 x 131072 bf16, gradient 456, two reads and one write, 7.0), by the vector
+// units on rows that leave lanes idle, by dependent loads and launches on few rows (1 x 131072 with 20 alternatives 12).
 #include "heads.hpp"
 #include "mx_parts.hpp"
 #include "rows.hpp"
