@@ -47,8 +47,9 @@ __device__ __forceinline__ float largest(const float (&x)[kRowUnit])
 }
 
 // A lane's sums on its way along a long row.  d = x c - q is one operation with q = m c rounded; what the rounding leaves, delta = q - m c, is made good in the
-// end: (x - m) c = d + delta.  Where m c is beyond fp32 (CAREFUL: rows of the lowest value, or of huge ones) d is (x - m) c.  T is kept for ENTROPY.
-constexpr float kFarOff = 1e38f;  // |m c| from here on is not for the quick form
+// end: (x - m) c = d + delta.  delta is up to half a step of q, of which 2^d and 2^delta bear no large ones: rows whose |m c| is 2^23 and more, where that half is more than
+// 1/4, are gone through again with d = (x - m) c (CAREFUL).  T is kept for ENTROPY.
+constexpr float kFarOff = 0x1p23f;
 template <bool CAREFUL, bool ENTROPY>
 struct Way {
     Sums a;
