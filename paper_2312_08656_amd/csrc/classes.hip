@@ -49,19 +49,21 @@ __device__ __forceinline__ float largest(const float (&x)[kRowUnit])
 // A lane's sums on its way along a long row.  d = x c - q is one operation with q = m c rounded; what the rounding leaves, delta = q - m c, is made good in the
 // end: (x - m) c = d + delta.  delta is up to half a step of q, of which 2^d and 2^delta bear no large ones: rows whose |m c| is 2^23 and more, where that half is more than
 // 1/4, are gone through again with d = (x - m) c (CAREFUL).  T is kept for ENTROPY.
-constexpr float kFarOff = 0x1p23f;
+// A lane whose own columns are all far below 0 (a mask of a large finite value) has q = -2^24 for theirs, of which 2^d is 0 or little: where the row's maximum is not far
+// off, they add nothing to it.
+constexpr float kFarOff = 0x1p23f, kFarDown = -0x1p24f;
 template <bool CAREFUL, bool ENTROPY>
 struct Way {
     Sums a;
     float q;
-    __device__ __forceinline__ void begin() { a = no_sums(), q = kLowest; }
+    __device__ __forceinline__ void begin() { a = no_sums(), q = kFarDown; }
     __device__ __forceinline__ void absorb(const float (&x)[kRowUnit], float top, float c)
     {
         const float m = fmaxf(a.m, top);
         if constexpr (CAREFUL) {
             move_to(a, m, c);
         } else {
-            const float to = fmaxf(m * c, kLowest), shift = fminf(to - q, kFar), f = exp2_of(-shift);
+            const float to = fmaxf(m * c, kFarDown), shift = fminf(to - q, kFar), f = exp2_of(-shift);
             if constexpr (ENTROPY) a.T = f * fmaf(-shift, a.S, a.T);
             a.S *= f;
             a.m = m;
@@ -77,7 +79,8 @@ struct Way {
     __device__ __forceinline__ Sums end(float c)
     {
         if constexpr (!CAREFUL) {
-            const float delta = fabsf(q) < kFarOff ? fmaf(-a.m, c, q) : 0.f, f = exp2_of(delta);
+            // (far up delta is anything: the row comes again.  Far down a NaN stays one)
+            const float delta = q > kFarDown ? fmaf(-a.m, c, q) : 0.f, f = q > kFarDown ? exp2_of(delta) : 0.f;
             if constexpr (ENTROPY) a.T = f * fmaf(delta, a.S, a.T);
             a.S *= f;
         }

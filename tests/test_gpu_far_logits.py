@@ -1,4 +1,4 @@
-"""Rows whose largest logit is far from 0, as it is or scaled by a small temperature, against 64 bits.
+"""Logits far from 0 beside ordinary ones, and rows whose largest logit is far from 0, against 64 bits: masks of a large finite value, small temperatures.
 
 Sizes are those of every way that a row of more than 8192 columns takes: cut among workgroups (few rows), held by one, and gone through by 256, 512 and 1024 threads."""
 import numpy as np
@@ -66,6 +66,54 @@ def check_distillation(x, at, temperature, gen):
     hc.close(loss[at], want, bound)
     maxk.maxk_distill_grad(x, data, index, dloss, grad, temperature)
     hc.close(grad[at], dx, dx_bound, x.dtype)
+
+
+def masked_rows(V, dtype, gen):
+    """Masks of a large finite value beside ordinary logits: at the row's start, its end, scattered over half of it, and over all but a few columns."""
+    col = torch.arange(V, device="cuda")
+    rows = []
+    for value in (-1e7, -1e8, -1e9, -1e10, -1e20, -1e30, torch.finfo(dtype).min):
+        for mask in (col < V * 3 // 100, col >= V - V * 3 // 100, torch.rand(V, generator=gen, device="cuda") < 0.5, (col + 1) % 4001 != 0):
+            row = 3 * torch.randn(V, generator=gen, device="cuda")
+            row[mask] = value
+            rows.append(row)
+    return torch.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("N,V", SIZES)
+def test_masks_of_a_large_finite_value(N, V, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(N + V)
+    for x, at in batches(masked_rows(V, dtype, gen), N, V, dtype, gen):
+        check_scores(x, at, gen)
+
+
+@pytest.mark.parametrize("temperature", [1.0, 2.0, 3.0, 5.0])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("N,V", SIZES)
+def test_masks_of_a_large_finite_value_in_distillation(N, V, dtype, temperature):
+    gen = torch.Generator(device="cuda").manual_seed(N + V)
+    for x, at in batches(masked_rows(V, dtype, gen), N, V, dtype, gen):
+        check_distillation(x, at, temperature, gen)
+
+
+def test_what_is_not_finite_beside_a_mask():
+    """A NaN whose lane has nothing else than masked columns still makes its row NaN; so does +Inf."""
+    for N, V in SIZES:
+        x = torch.zeros(max(N, 2), V, device="cuda")
+        x[:, V // 2:] = -1e30
+        x[0, V - 1], x[-1, V - 3] = float("nan"), float("inf")
+        for i in (0, x.shape[0] - 1):
+            y = x if N > 1 else x[i:i + 1].contiguous()
+            at = i if N > 1 else 0
+            logprob, entropy, dx = torch.zeros(y.shape[0], device="cuda"), torch.zeros(y.shape[0], device="cuda"), torch.zeros_like(y)
+            labels = torch.zeros(y.shape[0], dtype=torch.int32, device="cuda")
+            maxk.maxk_logprobs(y, labels, logprob, entropy)
+            assert torch.isnan(logprob[at]) and torch.isnan(entropy[at]), (N, V)
+            maxk.maxk_logprobs_grad(y, dx, labels, torch.ones(y.shape[0], device="cuda"))
+            assert torch.isnan(dx[at]).all(), (N, V)
+            if N > 2:
+                assert torch.isfinite(entropy[1:-1]).all() and torch.isfinite(dx[1:-1]).all()
 
 
 def far_rows(V, gen):
