@@ -366,7 +366,8 @@ MAXK_API maxk_status maxk_logprobs_grad(const void* d_logits, int32_t value_type
  *   loss[n] = sum_t q_t (log q_t - log p[index_t]),   dlogits[n,j] = dloss[n] / temperature (p_j - sum of q_t over the entries of column j).
  * An entry of -Inf, or whose column lies outside [0, V), is none; entries of one column each count.  A row without entries has loss 0 and no gradient; one whose logits
  * are all -Inf loss +Inf (0 without entries) and no gradient; q > 0 at a logit of -Inf gives loss +Inf and the formula's gradient.  maxk_distill_grad writes the loss too where d_loss
- * is given; dlogits may be the logits' own memory.  k is at most MAXK_DISTILL_MAX_K; temperature positive, it and its reciprocal within fp32's range.
+ * is given; dlogits may be the logits' own memory.  k is from 1 to V and at most MAXK_DISTILL_MAX_K; temperature positive, it and log2(e) / temperature within fp32's range
+ * (from 4.24e-39 on).  Differences of a row's logits that pass fp32's range count as infinite, and dloss / temperature has to be within it.
  * Workspace: maxk_classes_workspace(N, V, 0).
  */
 #define MAXK_DISTILL_MAX_K 1024

@@ -18,7 +18,7 @@ namespace maxk {
 namespace {
 
 constexpr int kThreads = 256;  // of a workgroup; T below: 256 or 1024
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kLn2 = 0.69314718055994531f;
 constexpr auto kNothing = [] {};
 constexpr float kFar = 256.f;  // 2^-256 is 0 in fp32: a difference past it need not be told, and is cut so that 0 times it stays 0
 

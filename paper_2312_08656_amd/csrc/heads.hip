@@ -26,6 +26,9 @@ bool bad_index(const void* p, int bytes, int V)
 
 bool bad_labels(const void* p, int bytes) { return p && ((bytes != 4 && bytes != 8) || !aligned(p, (size_t)bytes)); }
 
+// Logits are taken times log2 e / temperature in fp32: a factor of Inf makes a NaN of the largest one's difference, 0
+bool good_temperature(double t) { return t > 0.0 && isfinite((float)t) && isfinite((float)(1.0 / t) * kLog2e); }
+
 maxk_status classes(const ClassCall& C, int value_type, void* workspace, int64_t bytes, void* stream)
 {
     if (bad_values(C.logits, value_type) || (C.dlogits && bad_values(C.dlogits, value_type))) return MAXK_INVALID_ARGUMENT;
@@ -50,8 +53,7 @@ maxk_status logprobs(ClassCall C, int value_type, void* workspace, int64_t bytes
 
 maxk_status distill(ClassCall C, int value_type, double temperature, void* workspace, int64_t bytes, void* stream)
 {
-    if (bad_type(value_type) || bad_type(C.data_type) || !(temperature > 0.0) || !isfinite((float)(1.0 / temperature)) || (float)(1.0 / temperature) == 0.f)
-        return MAXK_INVALID_ARGUMENT;
+    if (bad_type(value_type) || bad_type(C.data_type) || !good_temperature(temperature)) return MAXK_INVALID_ARGUMENT;
     if (const maxk_status st = bad_rows(C.N, C.V, MAXK_MAX_CLASSES)) return st;
     if (C.k < 1 || C.k > C.V) return MAXK_INVALID_ARGUMENT;
     if (C.k > MAXK_DISTILL_MAX_K) return MAXK_UNSUPPORTED;

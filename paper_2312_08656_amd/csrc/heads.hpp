@@ -6,6 +6,7 @@
 namespace maxk {
 
 constexpr int kNormMaxDim = MAXK_NORM_MAX_DIM;
+constexpr float kLog2e = 1.44269504088896341f;
 
 struct NormCall {
     const void *X, *residual;  // residual: may be null, and H with it
