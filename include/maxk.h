@@ -317,7 +317,8 @@ MAXK_API maxk_status maxk_mx_matvec(const void* d_X, int32_t value_type, int64_t
  * stream.  MAXK_SCRATCH_TOO_SMALL where workspace_bytes is less than a call needs.
  *
  * Root-mean-square norm with the residual's addition:  H = X + residual (rounded to the format), r = 1 / sqrt(mean of a row's H^2 + eps),
- * Y[n,i] = H[n,i] r[n] gamma[i], of X [N x dim], gamma fp32 [dim], eps positive and finite.  d_residual and d_H are both given or both NULL (H is X then);
+ * Y[n,i] = H[n,i] r[n] gamma[i], of X [N x dim], gamma fp32 [dim], eps positive and finite, and r of a
+ * row of zeros, 1 / sqrt(eps), within fp32's range (eps from 8.64e-78 on).  d_residual and d_H are both given or both NULL (H is X then);
  * H may be X's or the residual's own memory.  Y leaves in X's format (d_Y; X's or the residual's memory too, where H is not there), in `format` as
  * maxk_mx_quantize would store its fp32 value (d_codes, d_scales), or both.  d_rstd (fp32 [N], r for the gradient) may be NULL.  dim is at most
  * MAXK_NORM_MAX_DIM.

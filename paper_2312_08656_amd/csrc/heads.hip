@@ -29,6 +29,9 @@ bool bad_labels(const void* p, int bytes) { return p && ((bytes != 4 && bytes !=
 // Logits are taken times log2 e / temperature in fp32: a factor of Inf makes a NaN of the largest one's difference, 0
 bool good_temperature(double t) { return t > 0.0 && isfinite((float)t) && isfinite((float)(1.0 / t) * kLog2e); }
 
+// r is fp32, and 1 / sqrt(eps) of a row of zeros: Inf there makes NaN of it
+bool good_eps(double eps) { return eps > 0.0 && isfinite(eps) && isfinite((float)(1.0 / sqrt(eps))); }
+
 maxk_status classes(const ClassCall& C, int value_type, void* workspace, int64_t bytes, void* stream)
 {
     if (bad_values(C.logits, value_type) || (C.dlogits && bad_values(C.dlogits, value_type))) return MAXK_INVALID_ARGUMENT;
@@ -70,7 +73,7 @@ extern "C" {
 MAXK_API maxk_status maxk_rms_norm(const void* d_X, const void* d_residual, int32_t value_type, int64_t N, int32_t dim, const float* d_gamma, double eps,
                                    void* d_H, void* d_Y, int32_t format, void* d_codes, uint8_t* d_scales, float* d_rstd, void* stream)
 {
-    if (bad_type(value_type) || !(eps > 0.0) || !isfinite(eps)) return MAXK_INVALID_ARGUMENT;
+    if (bad_type(value_type) || !good_eps(eps)) return MAXK_INVALID_ARGUMENT;
     if (const maxk_status st = bad_rows(N, dim, MAXK_NORM_MAX_DIM)) return st;
     if (N == 0) return MAXK_OK;
     if (!d_residual != !d_H || !d_codes != !d_scales || (!d_Y && !d_codes)) return MAXK_INVALID_ARGUMENT;

@@ -1,4 +1,4 @@
-"""Which temperatures distillation takes: those whose scales are numbers in fp32 (no device is touched)."""
+"""Which temperatures distillation and which eps the norm take: those whose scales and largest r are numbers in fp32 (no device is touched)."""
 import ctypes
 
 import numpy as np
@@ -32,3 +32,15 @@ def test_temperatures(lib):
         assert distill(lib, temperature) == INVALID, temperature
     for temperature in (4.241e-39, 1e-38, 1e-6, 1.0, 1e6, 1e38, top):
         assert distill(lib, temperature) == 0, temperature
+
+
+def norm(lib, eps):
+    return lib.maxk_rms_norm(p, None, 0, 0, 8, p, eps, None, p, 0, None, None, None, None)
+
+
+def test_eps(lib):
+    # of a row of zeros r = 1 / sqrt(eps): past fp32's range from eps = 2^-256 = 8.636e-78 down, and 0 r is not 0 there
+    for eps in (8.6e-78, 1e-80, 1e-100, 1e-300, 5e-324):
+        assert norm(lib, eps) == INVALID, eps
+    for eps in (8.7e-78, 1e-76, 1e-38, 1e-6, 1.0, 1e300):
+        assert norm(lib, eps) == 0, eps
