@@ -150,6 +150,10 @@ def _norm_backward(dY, dH, H, gamma, rstd, needs):
 class MaxKRMSNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tensor], eps: float):
+        if torch.is_autocast_enabled(X.device.type):
+            gamma = gamma.float() if gamma.dtype in _HALVES else gamma
+            if residual is not None and residual.dtype != X.dtype:
+                X, residual = (t.float() if t.dtype in _HALVES else t for t in (X, residual))
         X, gamma, residual = _norm_arguments(X, gamma, residual, "maxk_residual_norm")
         Y, rstd = torch.empty_like(X), torch.empty(X.shape[0], dtype=torch.float32, device=X.device)
         H = None if residual is None else torch.empty_like(X)
@@ -170,7 +174,8 @@ class MaxKRMSNorm(torch.autograd.Function):
 
 def maxk_residual_norm(X: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6):
     """Y = H r gamma with H = X + residual and r = 1 / sqrt(mean of a row's H^2 + eps): (Y, H), or Y alone where there is no residual.  X and residual [N, dim] in
-    float32, bfloat16 or float16, gamma float32 [dim]; differentiable (once) with respect to all three."""
+    float32, bfloat16 or float16, gamma float32 [dim]; differentiable (once) with respect to all three.  Under autocast an X and a residual of different types, and a
+    gamma in 16 bits, are taken in float32."""
     out = MaxKRMSNorm.apply(X, gamma, residual, eps)
     return out[0] if residual is None else out
 
