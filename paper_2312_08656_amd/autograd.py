@@ -288,5 +288,7 @@ class MaxKDistill(torch.autograd.Function):
 
 def maxk_distill_loss(logits: torch.Tensor, top_data: torch.Tensor, top_index: torch.Tensor, temperature: float = 1.0) -> torch.Tensor:
     """Divergence [N] (float32) of softmax(logits / temperature) from the softmax of a teacher's largest logits / temperature, as maxk_topk_cbsr or maxk_logprobs leaves
-    them: top_data [N, k] at the columns top_index [N, k].  Differentiable (once) with respect to the logits."""
+    them: top_data [N, k] at the columns top_index [N, k].  Differentiable (once) with respect to the logits; a top_data that requires a gradient is refused."""
+    if torch.is_grad_enabled() and top_data.requires_grad:
+        raise _b.MaxKError("maxk_distill_loss: there is no gradient of top_data: detach() it")
     return MaxKDistill.apply(logits, top_data, top_index, temperature)

@@ -1,4 +1,4 @@
-"""The norm under autograd, the library's calls replaced by plain torch on the host: operands that autocast mixes."""
+"""The norm and distillation under autograd, the library's calls replaced by plain torch on the host: operands that autocast mixes, and a teacher that wants a gradient."""
 import pytest
 import torch
 
@@ -28,7 +28,7 @@ def rms_norm_grad(dY, H, gamma, rstd, dX, dgamma=None, dH=None, workspace=None):
 
 @pytest.fixture
 def calls(monkeypatch):
-    for name, plain in (("maxk_rms_norm", rms_norm), ("maxk_rms_norm_grad", rms_norm_grad)):
+    for name, plain in (("maxk_rms_norm", rms_norm), ("maxk_rms_norm_grad", rms_norm_grad), ("maxk_distill", lambda logits, data, index, loss, t: loss.zero_())):
         # a kernel's writes are not on the tape, and autocast does not change what it computes
         monkeypatch.setattr(autograd._heads, name, torch.no_grad()(torch.autocast("cpu", enabled=False)(plain)))
 
@@ -85,3 +85,15 @@ def test_a_linear_map_and_a_residual_under_autocast_on_the_device(half):
     assert torch.equal(Y, Y2) and torch.equal(H, H2)
     got, want = torch.autograd.grad(Y.square().sum() + H.sum(), [h, gamma, R]), torch.autograd.grad(Y2.square().sum() + H2.sum(), wide)
     assert all(torch.equal(g, w.to(g.dtype)) for g, w in zip(got, want))
+
+
+def test_a_teacher_that_wants_a_gradient_is_refused(calls):
+    """The loss has none for it: what would be left out is said."""
+    logits, top = torch.zeros(3, 5, requires_grad=True), torch.zeros(3, 2, requires_grad=True)
+    index = torch.zeros(3, 2, dtype=torch.int32)
+    with pytest.raises(maxk.MaxKError, match="detach"):
+        maxk.maxk_distill_loss(logits, top, index)
+    assert maxk.maxk_distill_loss(logits, top.detach(), index).requires_grad
+    with torch.no_grad():
+        maxk.maxk_distill_loss(logits, top, index)
+    assert not maxk.maxk_distill_loss(logits.detach(), top.detach(), index).requires_grad
