@@ -301,7 +301,7 @@ MAXK_API maxk_status maxk_mx_input_grad_cbsr(const float* d_dXs, const void* d_s
 
 /*
  * The same product for few rows of X that are not rounded: Y[n,o] = bias[o] + sum_i X[n,i] W[o,i], X [N x din] in a MAXK_VALUE_* format, W [dout x din]
- * MAXK_MX_4, fp32 sums, Y [N x dout] in a MAXK_VALUE_* format of its own (rounded once).  16 rows cost about what one does; 17 to
+ * MAXK_MX_4, fp32 sums, Y [N x dout] in a MAXK_VALUE_* format of its own (rounded once).  16 rows cost up to twice what one does; 17 to
  * MAXK_MX_MATVEC_MAX_ROWS read W again for every 16 (more: MAXK_UNSUPPORTED).  dout is at most MAXK_MAX_CLASSES.  Of an fp32 X the bits below 2^-133 are
  * dropped; a row of X with an Inf or NaN has results that are not finite (which of them is not said) where W is not zero.  Codes behind column din have
  * to be those of zero, as maxk_mx_quantize leaves them.

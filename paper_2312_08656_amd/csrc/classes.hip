@@ -8,8 +8,10 @@
 // has its maximum and sums: a lane rescales its own when its maximum moves, lanes and wavefronts are joined in the end; the gradient reads the row again, from the caches, and
 // writes.  Few long rows are cut into segments, a workgroup each, whose sums a second launch joins.  Many short rows go through LDS, where a lane has one of them.
 //
-// Bound by memory from 64 columns on (169343 x 1000 fp32, distillation 251 us, 5.5 TB/s; 4096 x 131072 bf16, gradient 456, two reads and one write, 7.0), by the vector
-// units on rows that leave lanes idle, by dependent loads and launches on few rows (1 x 131072 with 20 alternatives 12).
+// Bound by memory: gradients from 64 columns on (169343 x 1000 fp32, distillation 251 us, 5.5 TB/s; 4096 x 131072 bf16 456, two reads and one write, 7.0) and, without
+// alternatives, forward calls on fp32 and on rows of some 5000 columns and more.  By the vector units: rows that leave lanes idle (40000 x 2500 bf16 forward 64, 39 at one
+// read), and alternatives, whose keys are sorted (16000 x 2500 bf16, 5 of them 53 and 50 of them 70, where the read takes 16).  By dependent loads and launches: few
+// rows (1 x 131072 with 20 alternatives 12).
 #include "heads.hpp"
 #include "mx_parts.hpp"
 #include "rows.hpp"
@@ -1642,7 +1644,9 @@ int threads_of(int V)
 // Segments of a row
 struct Cut { int segments, width; };
 constexpr int kLeastSegment = kThreads * kRowUnit;
-constexpr int kFewRows = 128;  // fewer are cut, up to 256 workgroups take 1024 threads a row
+constexpr int kFewRows = 128;        // fewer are cut
+constexpr int kRowsOf1024 = 512;     // of rows that are not held, up to so many have 1024 threads each,
+constexpr int kRowsOf512 = 1024;     // up to so many 512
 Cut cut_of(int64_t N, int V)
 {
     constexpr int kGroups = 512;
@@ -1729,19 +1733,26 @@ maxk_status run_classes(const ClassCall& C, void* workspace, hipStream_t s)
     if (units <= 64) return run_teams<VT, 64, 1, DISTILL, GRAD, TOP>(C, s);
     if (units <= 128) return run_teams<VT, 64, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 256) return run_teams<VT, 64, 4, DISTILL, GRAD, TOP>(C, s);
-    // Held and read once, or gone through twice?  us, held / gone through, gradient (alone): 40000 x 2500 bf16 104 (64) / 153 (99), fp32 149 (66) / 172 (100); 24396 x 4099 bf16 88 (54) /
-    // 124 (75); 12207 x 8192 bf16 75 (43) / 87 (44), fp32 143 / 178; 243 x 4099 4 / 6.  512 threads: 7142 x 14000 bf16 83 (42) / 95 (39), fp32 145 (68) / 190 (69);
-    // 4444 x 9000 bf16 with 5 alternatives 57 / 35, 20 61 / 55, 50 65 / 77, fp32 70 / 96, 2500 x 16000 bf16 44 / 60; 365 x 8200 gradient 7 (5) / 12 (8).  1024 threads: 3571 x 28000 bf16 125 / 101.
+    // Held and read once, or gone through twice?  us, held / gone through:
+    //   gradient (forward alone)                                       alternatives        5        20        24        50
+    //   40000 x 2500   bf16 104 (64) / 153 (99)  fp32 149 (66) / 172 (100)   16000 x 2500   bf16  53 / 67   60 / 87   61 / 93   70 / 146
+    //   24396 x 4099   bf16  88 (54) / 124 (75)                               9800 x 4099   bf16  40 / 44   46 / 56   47 / 59   52 / 89
+    //   12207 x 8192   bf16  75 (43) /  87 (44)  fp32 143      / 178          5000 x 8192   bf16  28 / 31   32 / 45   33 / 50   37 / 73
+    //     243 x 4099          4      /   6                                    (fp32 the same or more in favour of held)
+    // with 512 threads:
+    //    7142 x 14000  bf16  83 (42) /  95 (39)  fp32 145 (68) / 190 (69)     4444 x 9000   bf16  51 / 32   55 / 47   56 / 51   60 / 73   fp32  54 / 44   58 / 57   59 / 60   62 / 88
+    //     365 x 8200          7  (5) /  12  (8)                               2857 x 14000  bf16  39 / 30   43 / 43   43 / 44   46 / 64   fp32  43 / 44   47 / 52   47 / 55   50 / 76
+    // with 1024 threads: 3571 x 28000 bf16, gradient, 125 / 101.
     if (units <= 512) return run_held<VT, 256, 2, DISTILL, GRAD, TOP>(C, s);
     if (units <= 768) return run_held<VT, 256, 3, DISTILL, GRAD, TOP>(C, s);
     if (units <= 1024) return run_held<VT, 256, 4, DISTILL, GRAD, TOP>(C, s);
     const Cut cut = cut_of(C.N, C.V);
-    if (cut.segments == 1 && (GRAD || C.N <= 512 || C.top_k >= 24)) {
+    if (cut.segments == 1 && (GRAD || C.N <= kRowsOf1024 || C.top_k >= 24)) {
         if (units <= 1536) return run_held<VT, 512, 3, DISTILL, GRAD, TOP>(C, s);
         if (units <= 2048) return run_held<VT, 512, 4, DISTILL, GRAD, TOP>(C, s);
     }
     if (cut.segments == 1) {
-        const int T = C.N <= 512 ? 1024 : C.N <= 1024 ? 512 : GRAD ? threads_of<VT>(C.V) : kThreads;
+        const int T = C.N <= kRowsOf1024 ? 1024 : C.N <= kRowsOf512 ? 512 : GRAD ? threads_of<VT>(C.V) : kThreads;
         if (T == 1024) return run_rows<VT, 1024, DISTILL, GRAD, TOP>(C, s);
         if (T == 512) return run_rows<VT, 512, DISTILL, GRAD, TOP>(C, s);
         return run_rows<VT, kThreads, DISTILL, GRAD, TOP>(C, s);

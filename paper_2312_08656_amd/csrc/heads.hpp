@@ -5,7 +5,6 @@
 
 namespace maxk {
 
-constexpr int kNormMaxDim = MAXK_NORM_MAX_DIM;
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct NormCall {

@@ -7,8 +7,8 @@
 // stays in the Infinity Cache included; matrix instructions: 50); fp32 45.7 (83).
 //
 // More rows: matrix instructions take W as it decodes, exact in bf16, and X in bf16 parts that add up to it (three of fp32, two of fp16), so that products are
-// exact, and 2 to 16 rows cost the same.  A wavefront has 16 TILES rows of W and 512 columns at a time; the wavefronts of a workgroup share out the columns and
-// are joined in LDS.  The cutting of X takes the vector units 10 us of 16 rows of fp32 by 8192 x 8192, 19 in all, bf16 12.6 (W alone: 7); 16 rows of bf16, 4096 to 100003, 59.
+// exact, and 16 rows cost little more than three (4096 to 100003, us of 1, 2, 3 and 16 rows: fp32 48, 70, 81, 89, bf16 37, 48, 49, 59).  A wavefront has 16 TILES rows of W and
+// 512 columns at a time; the wavefronts of a workgroup share out the columns and are joined in LDS.  The cutting of X takes the vector units 10 us of 16 rows of fp32 by 8192 x 8192, 19 in all, bf16 12.6 (W alone: 7); 16 rows of bf16, 4096 to 100003, 59.
 #include "mx_parts.hpp"
 #include "rows.hpp"
 

@@ -60,7 +60,7 @@ def maxk_rms_norm(X: torch.Tensor, gamma: torch.Tensor, Y: Optional[torch.Tensor
                   rstd: Optional[torch.Tensor] = None, eps: float = 1e-6) -> None:
     """H = X + residual; Y = H r gamma with r = 1 / sqrt(mean of a row's H^2 + eps), X [N, dim], gamma [dim] float32.
 
-    Y is overwritten in X's type (Y), in 8 or 4 bits (codes and scales, see mx_empty), or both, rstd [N] with r.  residual and H are given together, and H may be either
+    Y is overwritten in X's type (Y), in 8 or 4 bits (codes and scales, see mx_empty), or both, rstd [N] with r.  eps is 8.64e-78 at least.  residual and H are given together, and H may be either
     operand itself; without them H is X."""
     what = "maxk_rms_norm"
     if _b._FAST is not None and _b._FAST.rms_norm(X, gamma, Y, codes, scales, residual, H, rstd, eps):
@@ -179,7 +179,8 @@ def _teacher(top_data: torch.Tensor, top_index: torch.Tensor, N: int, what: str)
 def maxk_distill(logits: torch.Tensor, top_data: torch.Tensor, top_index: torch.Tensor, loss: torch.Tensor, temperature: float = 1.0,
                  workspace: Optional[torch.Tensor] = None) -> None:
     """loss [N] is overwritten with the divergence of softmax(logits / temperature), logits [N, V], from the softmax of the k logits a row that a teacher passed on:
-    top_data [N, k] (any of the types) / temperature at the columns top_index [N, k] (uint8, uint16 or int32).  Entries of -inf or outside [0, V) are none."""
+    top_data [N, k] (any of the types) / temperature at the columns top_index [N, k] (uint8, uint16 or int32), k up to V and 1024.  Entries of -inf or outside [0, V) are
+    none.  temperature: from 4.24e-39 to fp32's largest value."""
     what = "maxk_distill"
     if _b._FAST is not None and _b._FAST.distill(logits, top_data, top_index, None, None, temperature, loss, workspace):
         return

@@ -112,7 +112,7 @@ def maxk_mx_linear(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch
 
 def maxk_mx_matvec(X: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, Y: torch.Tensor, bias: Optional[torch.Tensor] = None) -> None:
     """Y [N, dout] is overwritten with X W^T + bias for few rows X [N, din] that are not rounded, W [dout, din] in 4 bits; X and Y each float32, bfloat16
-    or float16.  16 rows cost about what one does."""
+    or float16.  16 rows cost up to twice what one does."""
     what = "maxk_mx_matvec"
     if _b._FAST is not None and _b._FAST.mx_matvec(X, w_codes, w_scales, Y, bias):
         return
